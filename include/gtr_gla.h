@@ -300,6 +300,132 @@ gtr_status_t gtr_gla_fwd_lowrank_gate(const void *q, const void *k, const void *
                                       gtr_scan_t scan_order, gtr_dtype_t dtype, void *out,
                                       float *final_state, cudaStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * The operators around the mixer in a pre-norm block: layer norm, the short
+ * causal convolution and the selective state-space scan (a second mixer, in the
+ * same scan orders), and the gated feed-forward step.  Argument rules in
+ * addition to the ones above: a token stride is the number of elements from one
+ * token (row) to the next, at least the row's length; float tensors (weights of
+ * the norm and the convolution, A, D, states of the scan, statistics) are
+ * contiguous float32; outputs overlap neither inputs nor one another.  All
+ * arithmetic is fp32 and outputs are rounded once; the sums of every call are
+ * made in a fixed order (the same bits every time).  None of these calls
+ * allocates device memory or synchronises (all are capturable), and none keeps
+ * anything between calls.
+ * ------------------------------------------------------------------------- */
+
+/* Layer norm over the last dimension: with m the mean of a row's D elements and
+ * r = 1 / sqrt(mean((x - m)^2) + eps),  out = (x - m) r weight + bias.
+ *   x: n rows of D elements of `dtype` at x_stride; weight, bias: [D] float32 or
+ *   NULL (ones, zeros); out: [n, D] contiguous; mean, rstd: [n] float32 or NULL
+ *   (what the backward pass reads).
+ * x and out 16-byte aligned; 1 <= D <= 16384; n >= 0 (0 launches nothing);
+ * eps >= 0.  D and x_stride multiples of 16 bytes run on 16-byte vectors. */
+gtr_status_t gtr_layernorm_fwd(const void *x, long long x_stride, const float *weight, const float *bias,
+                               float eps, long long n, int D, gtr_dtype_t dtype, void *out, float *mean,
+                               float *rstd, cudaStream_t stream);
+
+/* Bytes of workspace gtr_layernorm_bwd needs for dweight / dbias (partial sums). */
+size_t gtr_layernorm_bwd_workspace_bytes(long long n, int D);
+
+/* Backward pass of gtr_layernorm_fwd for the gradient dy [n rows of D at
+ * dy_stride, `dtype`] of its output: with xh = (x - mean) rstd and d = dy weight,
+ *   dx = rstd (d - mean_j(d) - xh mean_j(d xh)),
+ *   dweight = sum over rows of dy xh,  dbias = sum over rows of dy.
+ *   dx: [n, D] contiguous, `dtype`; dweight, dbias: [D] float32, each may be NULL
+ *   (not computed); mean, rstd: [n] float32, as the forward pass wrote them.
+ * workspace: 256-byte aligned, at least gtr_layernorm_bwd_workspace_bytes(n, D)
+ * (may be NULL when dweight and dbias are); GTR_ERR_WORKSPACE when it is missing
+ * or smaller.  Calls that overlap on the GPU must not share it.  n == 0 sets
+ * dweight and dbias to zero. */
+gtr_status_t gtr_layernorm_bwd(const void *dy, long long dy_stride, const void *x, long long x_stride,
+                               const float *weight, const float *mean, const float *rstd, long long n, int D,
+                               gtr_dtype_t dtype, void *dx, float *dweight, float *dbias, void *workspace,
+                               size_t workspace_bytes, cudaStream_t stream);
+
+/* Short causal depthwise convolution along a scan order (Sec. 3.1, directional
+ * scanning; T = grid_h * grid_w tokens in spatial row-major order, a plain
+ * sequence is grid_h = 1): with x_s the input at scan position s,
+ *   a_s = bias + sum_{j < W} weight[:, j] x_{s - W + 1 + j},  out_s = SiLU(a_s)
+ * (silu 1) or a_s (silu 0); out lies at the token of position s.
+ *   x: [B, T, E] at x_stride; weight: [E, W] float32; bias: [E] float32 or NULL;
+ *   initial_state: [B, W - 1, E] contiguous, `dtype`, the inputs at positions
+ *   -(W - 1) .. -1, or NULL (zeros); out: [B, T, E] contiguous; final_state:
+ *   [B, W - 1, E] contiguous or NULL, the inputs at the last W - 1 positions
+ *   (for T < W - 1 the initial state's last ones among them).
+ * 2 <= W <= 4, 1 <= E <= 2^20, T <= 2^30; x, out and the states 16-byte aligned. */
+gtr_status_t gtr_causal_conv_fwd(const void *x, long long x_stride, const float *weight, const float *bias,
+                                 int silu, const void *initial_state, int B, int grid_h, int grid_w, int E,
+                                 int W, gtr_scan_t scan_order, gtr_dtype_t dtype, void *out, void *final_state,
+                                 cudaStream_t stream);
+
+/* The next token of B sequences: x [B, E] at x_stride, state and state_out
+ * [B, W - 1, E] (state_out may be state: updated in place; a partial overlap is
+ * refused), out [B, E].  Other arguments as gtr_causal_conv_fwd, whose results
+ * for the longer sequence these are. */
+gtr_status_t gtr_causal_conv_step(const void *x, long long x_stride, const void *state, const float *weight,
+                                  const float *bias, int silu, int B, int E, int W, gtr_dtype_t dtype, void *out,
+                                  void *state_out, cudaStream_t stream);
+
+/* Selective state-space scan along a scan order, per channel e and state n:
+ *   dt = softplus(delta + delta_bias) (softplus 1) or delta + delta_bias (0),
+ *   h_s[e][n] = exp(dt A[e][n]) h_{s-1}[e][n] + dt x_s[e] Bm_s[n],
+ *   out_s[e] = (sum_n C_s[n] h_s[e][n] + D[e] x_s[e]) SiLU(z_s[e])
+ * with the D term and the gate left out where D or z is NULL.
+ *   x, delta, z: [B, T, E] of `dtype` at their token strides; Bm, C: [B, T, N] at
+ *   theirs (slices of one projection's output will do: these five need only their
+ *   elements' alignment); A: [E, N], D, delta_bias: [E] float32; initial_state:
+ *   [B, E, N] float32 or NULL (zeros); out: [B, T, E] contiguous; final_state:
+ *   [B, E, N] float32 or NULL (not written).
+ * 1 <= N <= 64, 1 <= E <= 2^20, T <= 2^30; out, A and the states 16-byte aligned.
+ * Meant for A < 0; a positive A grows the state as the formula says. */
+gtr_status_t gtr_ssm_scan_fwd(const void *x, long long x_stride, const void *delta, long long delta_stride,
+                              const float *A, const void *Bm, long long b_stride, const void *C,
+                              long long c_stride, const float *D, const void *z, long long z_stride,
+                              const float *delta_bias, int softplus, const float *initial_state, int B,
+                              int grid_h, int grid_w, int E, int N, gtr_scan_t scan_order, gtr_dtype_t dtype,
+                              void *out, float *final_state, cudaStream_t stream);
+
+/* The next token of B sequences: x, delta, z [B, E], Bm, C [B, N] at their
+ * strides, state and state_out [B, E, N] float32 (state_out may be state: updated
+ * in place; a partial overlap is refused), out [B, E].  Other arguments as
+ * gtr_ssm_scan_fwd. */
+gtr_status_t gtr_ssm_step(const void *x, long long x_stride, const void *delta, long long delta_stride,
+                          const float *A, const void *Bm, long long b_stride, const void *C, long long c_stride,
+                          const float *D, const void *z, long long z_stride, const float *delta_bias, int softplus,
+                          const float *state, int B, int E, int N, gtr_dtype_t dtype, void *out, float *state_out,
+                          cudaStream_t stream);
+
+/* Gated feed-forward step, both projections, the activation and the product in
+ * one kernel:  out = SiLU(x Wg^T) * (x Wv^T).
+ *   x: M tokens of D at x_stride; w_gate, w_value: [F, D] contiguous (rows are
+ *   output channels); out: [M, F] contiguous; all of one dtype, fp16 or bf16
+ *   (fp32 returns GTR_ERR_UNSUPPORTED).
+ * D, F and x_stride multiples of 8, all pointers 16-byte aligned, M >= 0 (0
+ * launches nothing).  A device-side wait that gives up is reported by
+ * gtr_gla_sync_status. */
+gtr_status_t gtr_swiglu_ffn_fwd(const void *x, long long x_stride, const void *w_gate, const void *w_value,
+                                long long M, int D, int F, gtr_dtype_t dtype, void *out, cudaStream_t stream);
+
+/* Bytes of workspace gtr_swiglu_ffn_bwd needs on the current device. */
+size_t gtr_swiglu_ffn_bwd_workspace_bytes(long long M, int D, int F);
+
+/* Backward pass of gtr_swiglu_ffn_fwd for the gradient dout [M, F at dout_stride]
+ * of its output; the projections G = x Wg^T and V = x Wv^T are computed again:
+ *   dV = dout SiLU(G),  dG = dout V s(G) (1 + G (1 - s(G))),
+ *   dx = dG Wg + dV Wv,  dw_gate = dG^T x,  dw_value = dV^T x
+ * (s the logistic function).  dG and dV are rounded to the dtype between the
+ * products, which take 16-bit operands; with fp16 keep dout scaled so that they
+ * stay in its range.  dx: [M, D], dw_gate, dw_value: [F, D], contiguous, of the
+ * inputs' dtype.  workspace: 256-byte aligned, at least
+ * gtr_swiglu_ffn_bwd_workspace_bytes(M, D, F), not shared by calls that overlap
+ * on the GPU; GTR_ERR_WORKSPACE when it is missing or smaller.  M == 0 sets the
+ * weights' gradients to zero. */
+gtr_status_t gtr_swiglu_ffn_bwd(const void *dout, long long dout_stride, const void *x, long long x_stride,
+                                const void *w_gate, const void *w_value, long long M, int D, int F,
+                                gtr_dtype_t dtype, void *dx, void *dw_gate, void *dw_value, void *workspace,
+                                size_t workspace_bytes, cudaStream_t stream);
+
 /* Size of the fixed device scratch array behind gtr_gla_fwd_noalloc.  The
  * library holds one such array on every GPU where it is loaded, from the
  * module's load until the process exits.  What a call keeps there is bounded by

@@ -1,0 +1,265 @@
+// block_api.cu -- the C ABI of the operators around the mixer (include/gtr_gla.h): layer norm, the
+// short causal convolution, the selective scan and the gated feed-forward step.  Argument validation
+// only; the kernels live in their own files.
+#include <cstdint>
+
+#include "gla_internal.h"
+#include "gtr_gla.h"
+
+namespace {
+
+constexpr long long kMaxTokens = 1LL << 30;
+constexpr long long kMaxExtent = 1LL << 40;  // elements a tensor may span
+
+bool at16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool at(const void *p, size_t align) { return (reinterpret_cast<uintptr_t>(p) & (align - 1)) == 0; }
+long long esize(int dtype) { return dtype == GTR_F32 ? 4 : 2; }
+bool dtype_ok(int dtype) { return dtype >= GTR_F32 && dtype <= GTR_BF16; }
+
+gtr_status_t done(cudaError_t e) {
+    if (e == cudaSuccess) return GTR_OK;
+    gtr::set_last_cuda_error(e);
+    return GTR_ERR_CUDA;
+}
+
+// A tensor's memory, `bytes` from `p` on (null or empty: none).
+struct Span {
+    const void *p;
+    long long bytes;
+};
+Span rows(const void *p, long long n, long long stride, long long width, long long es) {
+    return Span{p, n > 0 ? ((n - 1) * stride + width) * es : 0};
+}
+bool overlaps(const Span &a, const Span &b) {
+    if (!a.p || !b.p || a.bytes <= 0 || b.bytes <= 0) return false;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return x < y + static_cast<uintptr_t>(b.bytes) && y < x + static_cast<uintptr_t>(a.bytes);
+}
+// No output overlaps an input or another output.
+template <int NO, int NI> bool disjoint(const Span (&out)[NO], const Span (&in)[NI]) {
+    for (int i = 0; i < NO; ++i) {
+        for (int j = 0; j < NI; ++j)
+            if (overlaps(out[i], in[j])) return false;
+        for (int j = 0; j < i; ++j)
+            if (overlaps(out[i], out[j])) return false;
+    }
+    return true;
+}
+// n rows of `width` elements at `stride`: a legal stride, and offsets that stay far inside 64 bits.
+bool strided(long long n, long long stride, long long width) {
+    return stride >= width && stride <= kMaxExtent && (n == 0 || n <= kMaxExtent / stride);
+}
+
+gtr_status_t check_ln(long long n, int D, int dtype, long long x_stride) {
+    if (n < 0 || n > kMaxTokens || D < 1 || D > 16384 || !dtype_ok(dtype) || !strided(n, x_stride, D))
+        return GTR_ERR_INVALID_ARG;
+    return GTR_OK;
+}
+
+// Shape rules shared by the convolution and the scan.
+gtr_status_t check_seq(int B, int grid_h, int grid_w, int E, int order, int dtype) {
+    if (B < 0 || grid_h < 1 || grid_w < 1 || E < 1 || E > (1 << 20) || !dtype_ok(dtype)) return GTR_ERR_INVALID_ARG;
+    if (order < GTR_SCAN_ROW_FWD || order > GTR_SCAN_COL_REV) return GTR_ERR_INVALID_ARG;
+    const long long T = (long long)grid_h * grid_w;
+    if (T > kMaxTokens || (long long)B * T > kMaxExtent / E) return GTR_ERR_INVALID_ARG;
+    return GTR_OK;
+}
+
+gtr_status_t conv(const void *x, long long x_stride, const float *weight, const float *bias, const void *state_in, int B,
+                  int grid_h, int grid_w, int E, int W, int silu, int order, int dtype, void *out, void *state_out,
+                  bool step, cudaStream_t stream) {
+    gtr_status_t st = check_seq(B, grid_h, grid_w, E, order, dtype);
+    if (st != GTR_OK) return st;
+    const long long T = (long long)grid_h * grid_w, n = (long long)B * T, es = esize(dtype);
+    if (W < 2 || W > 4 || (silu != 0 && silu != 1) || !strided(n, x_stride, E)) return GTR_ERR_INVALID_ARG;
+    if (B == 0) return GTR_OK;
+    if (!x || !weight || !out || !at16(x) || !at16(out) || !at16(state_in) || !at16(state_out) || !at(weight, 4) ||
+        !at(bias, 4))
+        return GTR_ERR_INVALID_ARG;
+    if (step && (!state_in || !state_out)) return GTR_ERR_INVALID_ARG;
+    const Span state = rows(state_in, (long long)B * (W - 1), E, E, es);
+    const Span outs[2] = {rows(out, n, E, E, es), rows(state_out, (long long)B * (W - 1), E, E, es)};
+    // a step may move the state in its own memory
+    const Span ins[4] = {rows(x, n, x_stride, E, es), rows(weight, E, W, W, 4), rows(bias, bias ? 1 : 0, E, E, 4),
+                         step && state_out == state_in ? Span{nullptr, 0} : state};
+    if (!disjoint(outs, ins) || (step && overlaps(outs[0], state))) return GTR_ERR_INVALID_ARG;
+    const gtr::ConvProblem p{x, x_stride, weight, bias, state_in, out, state_out, B, grid_h, grid_w, E, W, order, silu, dtype};
+    return done(gtr::launch_conv(p, step, stream));
+}
+
+gtr_status_t ssm(const void *x, long long x_stride, const void *delta, long long delta_stride, const float *A,
+                 const void *Bm, long long b_stride, const void *C, long long c_stride, const float *D, const void *z,
+                 long long z_stride, const float *delta_bias, int softplus, const float *state_in, int B, int grid_h,
+                 int grid_w, int E, int N, int order, int dtype, void *out, float *state_out, bool step,
+                 cudaStream_t stream) {
+    gtr_status_t st = check_seq(B, grid_h, grid_w, E, order, dtype);
+    if (st != GTR_OK) return st;
+    const long long T = (long long)grid_h * grid_w, n = (long long)B * T, es = esize(dtype);
+    if (N < 1 || N > 64 || (softplus != 0 && softplus != 1)) return GTR_ERR_INVALID_ARG;
+    if (!strided(n, x_stride, E) || !strided(n, delta_stride, E) || !strided(n, b_stride, N) || !strided(n, c_stride, N) ||
+        (z && !strided(n, z_stride, E)))
+        return GTR_ERR_INVALID_ARG;
+    if (B == 0) return GTR_OK;
+    if (!x || !delta || !A || !Bm || !C || !out) return GTR_ERR_INVALID_ARG;
+    if (!at(x, es) || !at(delta, es) || !at(z, es) || !at(Bm, es) || !at(C, es) || !at16(out) || !at16(A) || !at(D, 4) ||
+        !at(delta_bias, 4) || !at16(state_in) || !at16(state_out))
+        return GTR_ERR_INVALID_ARG;
+    if (step && (!state_in || !state_out)) return GTR_ERR_INVALID_ARG;
+    const Span state = rows(state_in, (long long)B * E, N, N, 4);
+    const Span outs[2] = {rows(out, n, E, E, es), rows(state_out, (long long)B * E, N, N, 4)};
+    const Span ins[9] = {rows(x, n, x_stride, E, es), rows(delta, n, delta_stride, E, es),
+                         rows(z, n, z_stride, E, es), rows(Bm, n, b_stride, N, es),
+                         rows(C, n, c_stride, N, es), rows(A, E, N, N, 4),
+                         rows(D, 1, E, E, 4), rows(delta_bias, 1, E, E, 4),
+                         step && state_out == state_in ? Span{nullptr, 0} : state};
+    if (!disjoint(outs, ins) || (step && overlaps(outs[0], state))) return GTR_ERR_INVALID_ARG;
+    const gtr::SsmProblem p{x, delta, z, Bm, C, x_stride, delta_stride, z_stride, b_stride, c_stride, A, D, delta_bias,
+                            state_in, out, state_out, B, grid_h, grid_w, E, N, order, softplus, dtype};
+    return done(step ? gtr::launch_ssm_step(p, stream) : gtr::launch_ssm(p, stream));
+}
+
+// Shape rules of the feed-forward step: TMA wants rows of 16-byte multiples.
+gtr_status_t check_ffn(long long M, int D, int F, int dtype) {
+    if (M < 0 || M > kMaxTokens || D < 8 || F < 8 || D % 8 || F % 8 || !dtype_ok(dtype)) return GTR_ERR_INVALID_ARG;
+    if (D > (1 << 20) || F > (1 << 20) || M > kMaxExtent / D || M > kMaxExtent / F) return GTR_ERR_INVALID_ARG;
+    return dtype == GTR_F32 ? GTR_ERR_UNSUPPORTED : GTR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+gtr_status_t gtr_layernorm_fwd(const void *x, long long x_stride, const float *weight, const float *bias, float eps,
+                               long long n, int D, gtr_dtype_t dtype, void *out, float *mean, float *rstd,
+                               cudaStream_t stream) {
+    const gtr_status_t st = check_ln(n, D, dtype, x_stride);
+    if (st != GTR_OK) return st;
+    if (!(eps >= 0.f) || !(eps < 3.0e38f)) return GTR_ERR_INVALID_ARG;  // also rejects NaN
+    if (n == 0) return GTR_OK;
+    if (!x || !out || !at16(x) || !at16(out) || !at(weight, 4) || !at(bias, 4) || !at(mean, 4) || !at(rstd, 4))
+        return GTR_ERR_INVALID_ARG;
+    const long long es = esize(dtype);
+    const Span outs[3] = {rows(out, n, D, D, es), rows(mean, n, 1, 1, 4), rows(rstd, n, 1, 1, 4)};
+    const Span ins[3] = {rows(x, n, x_stride, D, es), rows(weight, 1, D, D, 4), rows(bias, 1, D, D, 4)};
+    if (!disjoint(outs, ins)) return GTR_ERR_INVALID_ARG;
+    const gtr::LnProblem p{x, x_stride, weight, bias, eps, n, D, dtype, out, mean, rstd};
+    return done(gtr::launch_layernorm(p, stream));
+}
+
+size_t gtr_layernorm_bwd_workspace_bytes(long long n, int D) {
+    if (check_ln(n, D, GTR_F32, D) != GTR_OK) return 0;
+    return gtr::layernorm_bwd_workspace(n, D);
+}
+
+gtr_status_t gtr_layernorm_bwd(const void *dy, long long dy_stride, const void *x, long long x_stride, const float *weight,
+                               const float *mean, const float *rstd, long long n, int D, gtr_dtype_t dtype, void *dx,
+                               float *dweight, float *dbias, void *workspace, size_t workspace_bytes, cudaStream_t stream) {
+    const gtr_status_t st = check_ln(n, D, dtype, x_stride);
+    if (st != GTR_OK) return st;
+    if (!strided(n, dy_stride, D) || !at(dweight, 4) || !at(dbias, 4) || !at(workspace, 256)) return GTR_ERR_INVALID_ARG;
+    if (n == 0) {  // sums over no rows
+        cudaError_t e = cudaSuccess;
+        if (dweight) e = cudaMemsetAsync(dweight, 0, (size_t)D * 4, stream);
+        if (e == cudaSuccess && dbias) e = cudaMemsetAsync(dbias, 0, (size_t)D * 4, stream);
+        return done(e);
+    }
+    if (!dy || !x || !mean || !rstd || !dx || !at16(dy) || !at16(x) || !at16(dx) || !at(weight, 4) || !at(mean, 4) ||
+        !at(rstd, 4))
+        return GTR_ERR_INVALID_ARG;
+    const size_t need = dweight || dbias ? gtr::layernorm_bwd_workspace(n, D) : 0;
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return GTR_ERR_WORKSPACE;
+    const long long es = esize(dtype);
+    const Span outs[4] = {rows(dx, n, D, D, es), rows(dweight, 1, D, D, 4), rows(dbias, 1, D, D, 4),
+                          Span{workspace, static_cast<long long>(need)}};
+    const Span ins[5] = {rows(dy, n, dy_stride, D, es), rows(x, n, x_stride, D, es), rows(weight, 1, D, D, 4),
+                         rows(mean, n, 1, 1, 4), rows(rstd, n, 1, 1, 4)};
+    if (!disjoint(outs, ins)) return GTR_ERR_INVALID_ARG;
+    const gtr::LnProblem p{x, x_stride, weight, nullptr, 0.f, n, D, dtype, dx, const_cast<float *>(mean),
+                           const_cast<float *>(rstd)};
+    return done(gtr::launch_layernorm_bwd(p, dy, dy_stride, dweight, dbias, workspace, stream));
+}
+
+gtr_status_t gtr_causal_conv_fwd(const void *x, long long x_stride, const float *weight, const float *bias, int silu,
+                                 const void *initial_state, int B, int grid_h, int grid_w, int E, int W,
+                                 gtr_scan_t scan_order, gtr_dtype_t dtype, void *out, void *final_state,
+                                 cudaStream_t stream) {
+    return conv(x, x_stride, weight, bias, initial_state, B, grid_h, grid_w, E, W, silu, scan_order, dtype, out,
+                final_state, false, stream);
+}
+
+gtr_status_t gtr_causal_conv_step(const void *x, long long x_stride, const void *state, const float *weight,
+                                  const float *bias, int silu, int B, int E, int W, gtr_dtype_t dtype, void *out,
+                                  void *state_out, cudaStream_t stream) {
+    return conv(x, x_stride, weight, bias, state, B, 1, 1, E, W, silu, GTR_SCAN_ROW_FWD, dtype, out, state_out, true,
+                stream);
+}
+
+gtr_status_t gtr_ssm_scan_fwd(const void *x, long long x_stride, const void *delta, long long delta_stride, const float *A,
+                              const void *Bm, long long b_stride, const void *C, long long c_stride, const float *D,
+                              const void *z, long long z_stride, const float *delta_bias, int softplus,
+                              const float *initial_state, int B, int grid_h, int grid_w, int E, int N,
+                              gtr_scan_t scan_order, gtr_dtype_t dtype, void *out, float *final_state,
+                              cudaStream_t stream) {
+    return ssm(x, x_stride, delta, delta_stride, A, Bm, b_stride, C, c_stride, D, z, z_stride, delta_bias, softplus,
+               initial_state, B, grid_h, grid_w, E, N, scan_order, dtype, out, final_state, false, stream);
+}
+
+gtr_status_t gtr_ssm_step(const void *x, long long x_stride, const void *delta, long long delta_stride, const float *A,
+                          const void *Bm, long long b_stride, const void *C, long long c_stride, const float *D,
+                          const void *z, long long z_stride, const float *delta_bias, int softplus, const float *state,
+                          int B, int E, int N, gtr_dtype_t dtype, void *out, float *state_out, cudaStream_t stream) {
+    return ssm(x, x_stride, delta, delta_stride, A, Bm, b_stride, C, c_stride, D, z, z_stride, delta_bias, softplus, state,
+               B, 1, 1, E, N, GTR_SCAN_ROW_FWD, dtype, out, state_out, true, stream);
+}
+
+gtr_status_t gtr_swiglu_ffn_fwd(const void *x, long long x_stride, const void *w_gate, const void *w_value, long long M,
+                                int D, int F, gtr_dtype_t dtype, void *out, cudaStream_t stream) {
+    const gtr_status_t st = check_ffn(M, D, F, dtype);
+    if (st != GTR_OK) return st;
+    if (!strided(M, x_stride, D) || x_stride % 8) return GTR_ERR_INVALID_ARG;
+    if (M == 0) return GTR_OK;
+    if (!x || !w_gate || !w_value || !out || !at16(x) || !at16(w_gate) || !at16(w_value) || !at16(out))
+        return GTR_ERR_INVALID_ARG;
+    const Span outs[1] = {rows(out, M, F, F, 2)};
+    const Span ins[3] = {rows(x, M, x_stride, D, 2), rows(w_gate, F, D, D, 2), rows(w_value, F, D, D, 2)};
+    if (!disjoint(outs, ins)) return GTR_ERR_INVALID_ARG;
+    const gtr::FfnProblem p{x, x_stride, w_gate, w_value, M, D, F, dtype};
+    if (!gtr::ffn_supported(p)) return GTR_ERR_UNSUPPORTED;
+    return done(gtr::launch_ffn(p, out, stream));
+}
+
+size_t gtr_swiglu_ffn_bwd_workspace_bytes(long long M, int D, int F) {
+    if (check_ffn(M, D, F, GTR_F16) != GTR_OK) return 0;
+    return gtr::ffn_bwd_workspace(M, F);
+}
+
+gtr_status_t gtr_swiglu_ffn_bwd(const void *dout, long long dout_stride, const void *x, long long x_stride,
+                                const void *w_gate, const void *w_value, long long M, int D, int F, gtr_dtype_t dtype,
+                                void *dx, void *dw_gate, void *dw_value, void *workspace, size_t workspace_bytes,
+                                cudaStream_t stream) {
+    const gtr_status_t st = check_ffn(M, D, F, dtype);
+    if (st != GTR_OK) return st;
+    if (!strided(M, x_stride, D) || x_stride % 8 || !strided(M, dout_stride, F) || dout_stride % 8) return GTR_ERR_INVALID_ARG;
+    if (!dw_gate || !dw_value || !at16(dw_gate) || !at16(dw_value) || !at(workspace, 256)) return GTR_ERR_INVALID_ARG;
+    const size_t nw = (size_t)F * D * 2;
+    if (M == 0) {  // sums over no tokens
+        if (overlaps(Span{dw_gate, (long long)nw}, Span{dw_value, (long long)nw})) return GTR_ERR_INVALID_ARG;
+        cudaError_t e = cudaMemsetAsync(dw_gate, 0, nw, stream);
+        if (e == cudaSuccess) e = cudaMemsetAsync(dw_value, 0, nw, stream);
+        return done(e);
+    }
+    if (!dout || !x || !w_gate || !w_value || !dx || !at16(dout) || !at16(x) || !at16(w_gate) || !at16(w_value) || !at16(dx))
+        return GTR_ERR_INVALID_ARG;
+    const size_t need = gtr::ffn_bwd_workspace(M, F);
+    if (workspace == nullptr || workspace_bytes < need) return GTR_ERR_WORKSPACE;
+    const Span outs[4] = {rows(dx, M, D, D, 2), rows(dw_gate, F, D, D, 2), rows(dw_value, F, D, D, 2),
+                          Span{workspace, static_cast<long long>(need)}};
+    const Span ins[4] = {rows(dout, M, dout_stride, F, 2), rows(x, M, x_stride, D, 2), rows(w_gate, F, D, D, 2),
+                         rows(w_value, F, D, D, 2)};
+    if (!disjoint(outs, ins)) return GTR_ERR_INVALID_ARG;
+    const gtr::FfnProblem p{x, x_stride, w_gate, w_value, M, D, F, dtype};
+    if (!gtr::ffn_supported(p)) return GTR_ERR_UNSUPPORTED;
+    return done(gtr::launch_ffn_bwd(p, dout, dout_stride, dx, dw_gate, dw_value, workspace, stream));
+}
+
+}  // extern "C"

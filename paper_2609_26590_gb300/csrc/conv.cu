@@ -1,0 +1,181 @@
+// conv.cu -- short causal depthwise convolution along a scan order, optionally followed by SiLU:
+//   a_s = b + sum_{j < W} w_j x_{s - W + 1 + j},  y_s = SiLU(a_s)
+// with the W - 1 inputs before the sequence zero or given, and the last W - 1 inputs returned as
+// the state from which single tokens go on.
+//
+// Memory-bound: each input is read once (and W - 1 again at the start of a strip, from L2), each
+// output written once.  A thread owns a 16-byte vector of channels (one channel where the
+// alignment does not allow vectors) and walks a strip of scan positions with the last W inputs
+// in registers; the scan order is in the walk's addresses.
+#include <cuda_runtime.h>
+
+#include "elem.cuh"
+#include "gla_internal.h"
+#include "scanpos.cuh"
+
+namespace gtr {
+namespace {
+
+constexpr int kConvThreads = 256;
+constexpr int kConvStrip = 16;  // scan positions a thread walks
+constexpr int kConvBatch = 4;   // loads in flight
+
+struct ConvParams {
+    const void *x;
+    long long x_stride;
+    const float *w, *b;
+    const void *init;
+    void *out, *state;
+    ScanGrid grid;
+    int B, E, silu, strips;
+    long long items;  // B * strips
+};
+
+template <typename E, int VEC, int W>
+__global__ void __launch_bounds__(kConvThreads) conv_kernel(const __grid_constant__ ConvParams p) {
+    const long long item = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+    const int c = (blockIdx.y * blockDim.x + threadIdx.x) * VEC;
+    if (item >= p.items || c >= p.E) return;
+    const int b = static_cast<int>(item / p.strips), strip = static_cast<int>(item - (long long)b * p.strips);
+    const int T = p.grid.T, s0 = strip * kConvStrip, s1 = T - s0 < kConvStrip ? T : s0 + kConvStrip;
+    const E *x = static_cast<const E *>(p.x) + (long long)b * T * p.x_stride + c;
+    const E *init = p.init ? static_cast<const E *>(p.init) + (long long)b * (W - 1) * p.E + c : nullptr;
+    E *out = static_cast<E *>(p.out) + (long long)b * T * p.E + c;
+    float w[W][VEC], bias[VEC], win[W][VEC];  // win: inputs s - W + 1 .. s
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        bias[i] = p.b ? p.b[c + i] : 0.f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[j][i] = p.w[(long long)(c + i) * W + j];
+    }
+    ScanPos pos;
+#pragma unroll
+    for (int j = 1; j < W; ++j) {  // inputs s0 - W + j
+        const int s = s0 - W + j;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) win[j][i] = 0.f;
+        if (s >= 0) {
+            pos.set(p.grid, s);
+            Vec<E, VEC>::unpack(ld_vec<E, VEC>(x + (long long)pos.t * p.x_stride), win[j]);
+        } else if (init) {
+            Vec<E, VEC>::unpack(ld_vec<E, VEC>(init + (long long)(s + W - 1) * p.E), win[j]);
+        }
+    }
+    pos.set(p.grid, s0);
+    for (int s = s0; s < s1; s += kConvBatch) {
+        typename Vec<E, VEC>::raw in[kConvBatch];
+        int tok[kConvBatch];
+#pragma unroll
+        for (int k = 0; k < kConvBatch; ++k) {
+            tok[k] = pos.t;
+            if (s + k < s1) {
+                in[k] = *reinterpret_cast<const typename Vec<E, VEC>::raw *>(x + (long long)pos.t * p.x_stride);
+                pos.next(p.grid);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kConvBatch; ++k) {
+            if (s + k >= s1) break;
+#pragma unroll
+            for (int j = 0; j + 1 < W; ++j)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) win[j][i] = win[j + 1][i];
+            Vec<E, VEC>::unpack(in[k], win[W - 1]);
+            float a[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                a[i] = bias[i];
+#pragma unroll
+                for (int j = 0; j < W; ++j) a[i] = fmaf(w[j][i], win[j][i], a[i]);
+                if (p.silu) a[i] = silu<E>(a[i]);
+            }
+            st_vec<E, VEC>(out + (long long)tok[k] * p.E, a);
+        }
+    }
+    if (p.state && s1 == T) {  // the window's last W - 1 inputs (exact: they are stored values)
+        E *st = static_cast<E *>(p.state) + (long long)b * (W - 1) * p.E + c;
+#pragma unroll
+        for (int j = 0; j + 1 < W; ++j) st_vec<E, VEC>(st + (long long)j * p.E, win[j + 1]);
+    }
+}
+
+// One token of every sequence: reads the state and the token, writes the output and the moved state
+// (which may be the state's own memory: a thread reads its channels before it writes them).
+template <typename E, int VEC, int W>
+__global__ void __launch_bounds__(kConvThreads) conv_step_kernel(const __grid_constant__ ConvParams p) {
+    const int b = blockIdx.x * blockDim.y + threadIdx.y;
+    const int c = (blockIdx.y * blockDim.x + threadIdx.x) * VEC;
+    if (b >= p.B || c >= p.E) return;
+    typename Vec<E, VEC>::raw in[W];
+    const E *init = static_cast<const E *>(p.init) + (long long)b * (W - 1) * p.E + c;
+#pragma unroll
+    for (int j = 0; j + 1 < W; ++j) in[j] = ld_vec<E, VEC>(init + (long long)j * p.E);
+    in[W - 1] = ld_vec<E, VEC>(static_cast<const E *>(p.x) + (long long)b * p.x_stride + c);
+    float a[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) a[i] = p.b ? p.b[c + i] : 0.f;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+        float f[VEC];
+        Vec<E, VEC>::unpack(in[j], f);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) a[i] = fmaf(p.w[(long long)(c + i) * W + j], f[i], a[i]);
+    }
+    if (p.silu) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) a[i] = silu<E>(a[i]);
+    }
+    st_vec<E, VEC>(static_cast<E *>(p.out) + (long long)b * p.E + c, a);
+    E *st = static_cast<E *>(p.state) + (long long)b * (W - 1) * p.E + c;
+#pragma unroll
+    for (int j = 0; j + 1 < W; ++j)
+        *reinterpret_cast<typename Vec<E, VEC>::raw *>(st + (long long)j * p.E) = in[j + 1];
+}
+
+template <typename E, int VEC, int W> cudaError_t conv_run(ConvParams &p, bool step, cudaStream_t stream) {
+    const int nv = (p.E + VEC - 1) / VEC;
+    int ny = (nv + kConvThreads - 1) / kConvThreads;
+    const int bx = (nv + ny - 1) / ny, by = kConvThreads / bx;  // bx <= 256
+    const long long rows = step ? p.B : p.items, gx = (rows + by - 1) / by;
+    if (gx > 0x7fffffffLL || ny > 65535) return cudaErrorInvalidValue;
+    const dim3 grid(static_cast<unsigned>(gx), ny), block(bx, by);
+    if (step)
+        conv_step_kernel<E, VEC, W><<<grid, block, 0, stream>>>(p);
+    else
+        conv_kernel<E, VEC, W><<<grid, block, 0, stream>>>(p);
+    return cudaGetLastError();
+}
+template <typename E, int VEC> cudaError_t conv_run_w(ConvParams &p, int W, bool step, cudaStream_t s) {
+    if (W == 2) return conv_run<E, VEC, 2>(p, step, s);
+    if (W == 3) return conv_run<E, VEC, 3>(p, step, s);
+    return conv_run<E, VEC, 4>(p, step, s);
+}
+template <typename E> cudaError_t conv_run_e(ConvParams &p, int W, bool step, cudaStream_t s) {
+    constexpr int V = 16 / static_cast<int>(sizeof(E));
+    if (p.E % V == 0 && p.x_stride % V == 0) return conv_run_w<E, V>(p, W, step, s);
+    return conv_run_w<E, 1>(p, W, step, s);
+}
+
+}  // namespace
+
+cudaError_t launch_conv(const ConvProblem &q, bool step, cudaStream_t stream) {
+    ConvParams p;
+    p.x = q.x;
+    p.x_stride = q.x_stride;
+    p.w = q.weight;
+    p.b = q.bias;
+    p.init = q.state_in;
+    p.out = q.out;
+    p.state = q.state_out;
+    p.grid = make_scan_grid(q.grid_h, q.grid_w, q.order);
+    p.B = q.B;
+    p.E = q.E;
+    p.silu = q.silu;
+    p.strips = (p.grid.T - 1) / kConvStrip + 1;
+    p.items = (long long)q.B * p.strips;
+    if (q.dtype == 0) return conv_run_e<float>(p, q.W, step, stream);
+    if (q.dtype == 1) return conv_run_e<__half>(p, q.W, step, stream);
+    return conv_run_e<__nv_bfloat16>(p, q.W, step, stream);
+}
+
+}  // namespace gtr

@@ -1,0 +1,80 @@
+// elem.cuh -- storage types (fp32, fp16, bf16) read and written as fp32 values, one or
+// 16 bytes at a time, and the activations that the block's kernels share.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cstdint>
+
+namespace gtr {
+
+__device__ __forceinline__ float to_f32(float a) { return a; }
+__device__ __forceinline__ float to_f32(__half a) { return __half2float(a); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 a) { return __bfloat162float(a); }
+template <typename E> __device__ __forceinline__ E from_f32(float a);
+template <> __device__ __forceinline__ float from_f32<float>(float a) { return a; }
+template <> __device__ __forceinline__ __half from_f32<__half>(float a) { return __float2half_rn(a); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float a) { return __float2bfloat16_rn(a); }
+
+// Two neighbouring 16-bit values in a word, the lower address in the lower half.
+template <typename E> __device__ __forceinline__ float2 unpack16(uint32_t w);
+template <> __device__ __forceinline__ float2 unpack16<__half>(uint32_t w) {
+    return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+}
+template <> __device__ __forceinline__ float2 unpack16<__nv_bfloat16>(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+template <typename E> __device__ __forceinline__ uint32_t pack16(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack16<__half>(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pack16<__nv_bfloat16>(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// VEC consecutive elements: 1, or the 16 bytes of an aligned vector.
+template <typename E, int VEC> struct Vec;
+template <typename E> struct Vec<E, 1> {
+    using raw = E;
+    static __device__ __forceinline__ void unpack(const raw &r, float (&f)[1]) { f[0] = to_f32(r); }
+    static __device__ __forceinline__ raw pack(const float (&f)[1]) { return from_f32<E>(f[0]); }
+};
+template <> struct Vec<float, 4> {
+    using raw = float4;
+    static __device__ __forceinline__ void unpack(const raw &r, float (&f)[4]) {
+        f[0] = r.x, f[1] = r.y, f[2] = r.z, f[3] = r.w;
+    }
+    static __device__ __forceinline__ raw pack(const float (&f)[4]) { return make_float4(f[0], f[1], f[2], f[3]); }
+};
+template <typename E> struct Vec<E, 8> {
+    using raw = uint4;
+    static __device__ __forceinline__ void unpack(const raw &r, float (&f)[8]) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = unpack16<E>(w[i]);
+            f[2 * i] = a.x, f[2 * i + 1] = a.y;
+        }
+    }
+    static __device__ __forceinline__ raw pack(const float (&f)[8]) {
+        return make_uint4(pack16<E>(f[0], f[1]), pack16<E>(f[2], f[3]), pack16<E>(f[4], f[5]), pack16<E>(f[6], f[7]));
+    }
+};
+template <typename E, int VEC> __device__ __forceinline__ typename Vec<E, VEC>::raw ld_vec(const E *p) {
+    return *reinterpret_cast<const typename Vec<E, VEC>::raw *>(p);
+}
+template <typename E, int VEC> __device__ __forceinline__ void st_vec(E *p, const float (&f)[VEC]) {
+    *reinterpret_cast<typename Vec<E, VEC>::raw *>(p) = Vec<E, VEC>::pack(f);
+}
+
+// SiLU(z) = z / (1 + e^{-z}).  16-bit outputs take the hardware's power and reciprocal (a few
+// 2^-22 of the value); fp32 outputs the library's exponential and an exact division.
+template <typename E> __device__ __forceinline__ float silu(float z) {
+    return __fdividef(z, 1.f + __expf(-z));
+}
+template <> __device__ __forceinline__ float silu<float>(float z) { return z / (1.f + expf(-z)); }
+
+}  // namespace gtr

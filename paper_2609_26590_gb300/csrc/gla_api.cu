@@ -204,6 +204,10 @@ gtr_status_t dispatch(const gtr::Problem &p, gtr_schedule_t schedule, void *ws, 
 
 }  // namespace
 
+namespace gtr {
+void set_last_cuda_error(cudaError_t e) { t_last_cuda_error = static_cast<int>(e); }
+}  // namespace gtr
+
 extern "C" {
 
 gtr_status_t gtr_gla_fwd_sched(const void *q, const void *k, const void *v, const void *log_gate,
@@ -492,12 +496,14 @@ gtr_status_t gtr_gla_fwd_host(const void *q_host, const void *k_host, const void
 gtr_status_t gtr_gla_sync_status(cudaStream_t stream) {
     cudaError_t e = cudaStreamSynchronize(stream);
     if (e != cudaSuccess) return cuda_fail(e);
-    unsigned int word = 0, sw = 0;
+    unsigned int word = 0, sw = 0, ffn = 0;
     e = gtr::read_and_clear_device_status(&word);
     if (e != cudaSuccess) return cuda_fail(e);
     e = gtr::read_and_clear_sswiglu_status(&sw);
     if (e != cudaSuccess) return cuda_fail(e);
-    if ((word | sw) & gtr::kStatusTimeout) return GTR_ERR_TIMEOUT;
+    e = gtr::read_and_clear_ffn_status(&ffn);
+    if (e != cudaSuccess) return cuda_fail(e);
+    if ((word | sw | ffn) & gtr::kStatusTimeout) return GTR_ERR_TIMEOUT;
     return GTR_OK;
 }
 

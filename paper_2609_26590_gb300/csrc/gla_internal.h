@@ -114,6 +114,77 @@ cudaError_t launch_sswiglu(const SwProblem &p, cudaStream_t stream);
 // Status word of the S-SwiGLU kernel's bounded wait (kStatusTimeout).
 cudaError_t read_and_clear_sswiglu_status(unsigned int *status);
 
+// Layer norm over rows of D elements and its backward pass (layernorm.cu).
+struct LnProblem {
+    const void *x;          // [rows] at x_stride elements
+    long long x_stride;
+    const float *weight;    // [D] or null (ones)
+    const float *bias;      // [D] or null (zeros); forward only
+    float eps;              // forward only
+    long long rows;
+    int D;
+    int dtype;              // 0 f32, 1 f16, 2 bf16
+    void *out;              // [rows, D]: y, or dx
+    float *mean, *rstd;     // [rows]: written (or null) by the forward pass, read by the backward
+};
+cudaError_t launch_layernorm(const LnProblem &p, cudaStream_t stream);
+// Scratch of the backward pass: one partial row of dw and db a CTA.
+size_t layernorm_bwd_workspace(long long rows, int D);
+// dweight and dbias may be null; with both null the workspace is not used.
+cudaError_t launch_layernorm_bwd(const LnProblem &p, const void *dy, long long dy_stride, float *dweight, float *dbias,
+                                 void *workspace, cudaStream_t stream);
+
+// Short causal convolution along a scan order, or one token of every sequence (conv.cu).
+struct ConvProblem {
+    const void *x;          // [B, T, E] at x_stride elements a token; a step: [B, E]
+    long long x_stride;
+    const float *weight;    // [E, W]
+    const float *bias;      // [E] or null
+    const void *state_in;   // [B, W - 1, E] or null (zeros); a step: not null
+    void *out;              // [B, T, E]
+    void *state_out;        // [B, W - 1, E] or null; a step: not null, may be state_in
+    int B, grid_h, grid_w, E, W, order, silu;
+    int dtype;
+};
+cudaError_t launch_conv(const ConvProblem &p, bool step, cudaStream_t stream);
+
+// Selective state-space scan along a scan order, or one token of every sequence (ssm.cu).
+struct SsmProblem {
+    const void *x, *delta, *z;         // [B, T, E] at their strides a token; z may be null
+    const void *Bm, *C;                // [B, T, N]
+    long long x_stride, delta_stride, z_stride, b_stride, c_stride;
+    const float *A;                    // [E, N]
+    const float *D, *delta_bias;       // [E] or null
+    const float *state_in;             // [B, E, N] or null (zeros); a step: not null
+    void *out;                         // [B, T, E]
+    float *state_out;                  // [B, E, N] or null; a step: not null, may be state_in
+    int B, grid_h, grid_w, E, N, order, softplus;
+    int dtype;
+};
+cudaError_t launch_ssm(const SsmProblem &p, cudaStream_t stream);
+cudaError_t launch_ssm_step(const SsmProblem &p, cudaStream_t stream);
+
+// Gated feed-forward step and its backward pass (ffn.cu).
+struct FfnProblem {
+    const void *x;                 // [M, D] at x_stride elements
+    long long x_stride;
+    const void *w_gate, *w_value;  // [F, D]
+    long long M;
+    int D, F;
+    int dtype;                     // 1 f16, 2 bf16
+};
+bool ffn_supported(const FfnProblem &p);
+cudaError_t launch_ffn(const FfnProblem &p, void *out, cudaStream_t stream);
+// Scratch of the backward pass: dG and dV.
+size_t ffn_bwd_workspace(long long M, int F);
+cudaError_t launch_ffn_bwd(const FfnProblem &p, const void *dout, long long dout_stride, void *dx, void *dw_gate,
+                           void *dw_value, void *workspace, cudaStream_t stream);
+// Status word of its bounded waits (kStatusTimeout).
+cudaError_t read_and_clear_ffn_status(unsigned int *status);
+
+// Keeps the error behind a GTR_ERR_CUDA for gtr_last_cuda_error (gla_api.cu).
+void set_last_cuda_error(cudaError_t e);
+
 enum : unsigned int { kStatusTimeout = 1u };
 
 }  // namespace gtr

@@ -95,6 +95,28 @@ def load(path: Optional[str] = None):
         lib.gtr_gla_fwd_lowrank_gate.argtypes = [vp] * 6 + [ctypes.c_float] + [ci] * 9 + [vp, vp, vp]
         lib.gtr_gla_last_schedule.restype = ci
         lib.gtr_gla_last_schedule.argtypes = [ctypes.POINTER(ci)] * 2
+        ll, cf = ctypes.c_longlong, ctypes.c_float
+        lib.gtr_layernorm_fwd.restype = ci
+        lib.gtr_layernorm_fwd.argtypes = [vp, ll, vp, vp, cf, ll, ci, ci, vp, vp, vp, vp]
+        lib.gtr_layernorm_bwd_workspace_bytes.restype = st
+        lib.gtr_layernorm_bwd_workspace_bytes.argtypes = [ll, ci]
+        lib.gtr_layernorm_bwd.restype = ci
+        lib.gtr_layernorm_bwd.argtypes = [vp, ll, vp, ll, vp, vp, vp, ll, ci, ci, vp, vp, vp, vp, st, vp]
+        lib.gtr_causal_conv_fwd.restype = ci
+        lib.gtr_causal_conv_fwd.argtypes = [vp, ll, vp, vp, ci, vp] + [ci] * 7 + [vp, vp, vp]
+        lib.gtr_causal_conv_step.restype = ci
+        lib.gtr_causal_conv_step.argtypes = [vp, ll, vp, vp, vp, ci] + [ci] * 4 + [vp, vp, vp]
+        lib.gtr_ssm_scan_fwd.restype = ci
+        lib.gtr_ssm_scan_fwd.argtypes = [vp, ll, vp, ll, vp, vp, ll, vp, ll, vp, vp, ll, vp, ci, vp] + [ci] * 7 + [
+            vp, vp, vp]
+        lib.gtr_ssm_step.restype = ci
+        lib.gtr_ssm_step.argtypes = [vp, ll, vp, ll, vp, vp, ll, vp, ll, vp, vp, ll, vp, ci, vp] + [ci] * 4 + [vp, vp, vp]
+        lib.gtr_swiglu_ffn_fwd.restype = ci
+        lib.gtr_swiglu_ffn_fwd.argtypes = [vp, ll, vp, vp, ll, ci, ci, ci, vp, vp]
+        lib.gtr_swiglu_ffn_bwd_workspace_bytes.restype = st
+        lib.gtr_swiglu_ffn_bwd_workspace_bytes.argtypes = [ll, ci, ci]
+        lib.gtr_swiglu_ffn_bwd.restype = ci
+        lib.gtr_swiglu_ffn_bwd.argtypes = [vp, ll, vp, ll, vp, vp, ll, ci, ci, ci, vp, vp, vp, vp, st, vp]
         if path is None:
             _lib = lib
         return lib
@@ -408,6 +430,310 @@ def forward_lowrank_gate(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, a_lo
         fs.data_ptr() if fs is not None else None, _stream_ptr(stream))
     _check(status, "gtr_gla_fwd_lowrank_gate", lib)
     return out, fs
+
+
+# ------------------------------------------------------------------ the operators around the mixer
+#
+# Outputs and workspaces that a call allocates belong to the stream it runs on (``stream``, else the
+# current one), so the caching allocator hands their memory on only behind that stream's work.
+
+
+def _code(t: torch.Tensor) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"unsupported dtype {t.dtype}")
+    return code
+
+
+def _on_device(first: torch.Tensor, **tensors) -> None:
+    """Every tensor lies on the current CUDA device (kernels and allocations go there)."""
+    for name, t in tensors.items():
+        if t is not None and (not t.is_cuda or t.device != first.device):
+            raise ValueError(f"{name} must be a CUDA tensor on the other inputs' device")
+    if first.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"the tensors are on {first.device}, which is not the current device")
+
+
+def _like(t: torch.Tensor, dtype: torch.dtype, shape, name: str) -> None:
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} {str(dtype).split('.')[1]} tensor")
+
+
+def _new(given: Optional[torch.Tensor], shape, dtype: torch.dtype, device, stream, name: str) -> torch.Tensor:
+    """The caller's tensor, checked, or a new one whose memory belongs to the call's stream."""
+    if given is not None:
+        _like(given, dtype, shape, name)
+        if given.device != device:
+            raise ValueError(f"{name} must be on the inputs' device")
+        return given
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _row_stride(t: torch.Tensor, name: str) -> int:
+    """Elements from one row (all leading dimensions flattened) to the next; the last dimension is
+    contiguous and the leading ones collapse into one."""
+    width, n = t.shape[-1], t.numel() // max(t.shape[-1], 1)
+    if width != 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    stride = span = None
+    for size, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if stride is None:
+            stride = st
+        elif st != span:
+            raise ValueError(f"{name}'s leading dimensions must collapse into one token stride")
+        span = st * size
+    if stride is None or n <= 1:
+        return width
+    if stride < width:
+        raise ValueError(f"{name}'s tokens overlap")
+    return stride
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return t.data_ptr() if t is not None else None
+
+
+def layernorm(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], eps: float,
+              stats: bool = False, out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Layer norm over the last dimension through ``gtr_layernorm_fwd``.  x: [..., D] (contiguous last
+    dimension, one token stride); weight, bias: [D] float32 or None.  Returns out like x (contiguous), with
+    ``stats`` (out, mean, rstd): float32 of x's leading shape, what :func:`layernorm_backward` reads."""
+    lib, code = load(), _code(x)
+    D, dev = x.shape[-1], x.device
+    _on_device(x, x=x, weight=weight, bias=bias)
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is not None:
+            _like(t, torch.float32, (D,), name)
+    xs = _row_stride(x, "x")
+    out = _new(out, x.shape, x.dtype, dev, stream, "out")
+    mean = rstd = None
+    if stats:
+        mean = _new(None, x.shape[:-1], torch.float32, dev, stream, "mean")
+        rstd = _new(None, x.shape[:-1], torch.float32, dev, stream, "rstd")
+    status = lib.gtr_layernorm_fwd(x.data_ptr(), xs, _ptr(weight), _ptr(bias), float(eps), x.numel() // max(D, 1), D, code,
+                                   out.data_ptr(), _ptr(mean), _ptr(rstd), _stream_ptr(stream))
+    _check(status, "gtr_layernorm_fwd", lib)
+    return (out, mean, rstd) if stats else out
+
+
+def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
+                       rstd: torch.Tensor, stream: Optional[torch.cuda.Stream] = None,
+                       workspace: Optional[torch.Tensor] = None):
+    """Backward pass of :func:`layernorm` through ``gtr_layernorm_bwd``: (dx, dweight, dbias) for the gradient
+    dy of its output; dweight and dbias ([D] float32) are None when weight is None.  ``workspace``: a CUDA uint8
+    tensor of at least ``layernorm_backward_workspace_bytes()`` that no overlapping call shares."""
+    lib, code = load(), _code(x)
+    D, dev = x.shape[-1], x.device
+    _on_device(x, x=x, dy=dy, weight=weight, mean=mean, rstd=rstd, workspace=workspace)
+    if dy.shape != x.shape or dy.dtype != x.dtype:
+        raise ValueError("dy must have x's shape and dtype")
+    if weight is not None:
+        _like(weight, torch.float32, (D,), "weight")
+    _like(mean, torch.float32, x.shape[:-1], "mean")
+    _like(rstd, torch.float32, x.shape[:-1], "rstd")
+    xs, ds, n = _row_stride(x, "x"), _row_stride(dy, "dy"), x.numel() // max(D, 1)
+    dx = _new(None, x.shape, x.dtype, dev, stream, "dx")
+    dw = db = None
+    if weight is not None:
+        dw = _new(None, (D,), torch.float32, dev, stream, "dweight")
+        db = _new(None, (D,), torch.float32, dev, stream, "dbias")
+        if workspace is None:
+            workspace = _new(None, (layernorm_backward_workspace_bytes(n, D),), torch.uint8, dev, stream, "workspace")
+    status = lib.gtr_layernorm_bwd(dy.data_ptr(), ds, x.data_ptr(), xs, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), n, D,
+                                   code, dx.data_ptr(), _ptr(dw), _ptr(db), _ptr(workspace), _nbytes(workspace),
+                                   _stream_ptr(stream))
+    _check(status, "gtr_layernorm_bwd", lib)
+    return dx, dw, db
+
+
+def _nbytes(t: Optional[torch.Tensor]) -> int:
+    return t.numel() * t.element_size() if t is not None else 0
+
+
+def layernorm_backward_workspace_bytes(n: int, D: int) -> int:
+    """Device workspace ``layernorm_backward`` needs for n rows of D."""
+    return int(load().gtr_layernorm_bwd_workspace_bytes(n, D))
+
+
+def _sequence(x, grid_h, grid_w):
+    if x.dim() != 3 or x.shape[1] != grid_h * grid_w:
+        raise ValueError("x must be [B, T, E] with T = grid_h * grid_w")
+    return x.shape
+
+
+def causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor], grid_h: int, grid_w: int,
+                order: int = ROW_FWD, silu: bool = True, initial_state: Optional[torch.Tensor] = None, final_state=False,
+                out: Optional[torch.Tensor] = None,
+                stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Short causal depthwise convolution along a scan order, then SiLU, through ``gtr_causal_conv_fwd``.
+    x: [B, T, E]; weight: [E, W] float32 (W 2 to 4, the last tap on the current token); bias: [E] float32 or None;
+    initial_state: [B, W - 1, E] like x or None.  ``final_state``: True (allocate), None/False (skip) or a
+    [B, W - 1, E] tensor.  Returns (out, final_state)."""
+    lib, code = load(), _code(x)
+    B, T, E = _sequence(x, grid_h, grid_w)
+    W = weight.shape[-1]
+    _on_device(x, x=x, weight=weight, bias=bias, initial_state=initial_state)
+    _like(weight, torch.float32, (E, W), "weight")
+    if bias is not None:
+        _like(bias, torch.float32, (E,), "bias")
+    if initial_state is not None:
+        _like(initial_state, x.dtype, (B, W - 1, E), "initial_state")
+    xs = _row_stride(x, "x")
+    out = _new(out, (B, T, E), x.dtype, x.device, stream, "out")
+    fs = None
+    if final_state is not None and final_state is not False:
+        fs = _new(None if final_state is True else final_state, (B, W - 1, E), x.dtype, x.device, stream, "final_state")
+    status = lib.gtr_causal_conv_fwd(x.data_ptr(), xs, weight.data_ptr(), _ptr(bias), int(bool(silu)), _ptr(initial_state),
+                                     B, grid_h, grid_w, E, W, order, code, out.data_ptr(), _ptr(fs), _stream_ptr(stream))
+    _check(status, "gtr_causal_conv_fwd", lib)
+    return out, fs
+
+
+def causal_conv_step(x: torch.Tensor, state: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor],
+                     silu: bool = True, state_out: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The next token of every sequence through ``gtr_causal_conv_step``.  x: [B, E]; state: [B, W - 1, E], updated
+    in place unless ``state_out`` is given.  Returns (out, the new state)."""
+    lib, code = load(), _code(x)
+    if x.dim() != 2:
+        raise ValueError("x must be [B, E]")
+    B, E = x.shape
+    W = weight.shape[-1]
+    _on_device(x, x=x, state=state, weight=weight, bias=bias)
+    _like(weight, torch.float32, (E, W), "weight")
+    if bias is not None:
+        _like(bias, torch.float32, (E,), "bias")
+    _like(state, x.dtype, (B, W - 1, E), "state")
+    new = _new(state if state_out is None else state_out, state.shape, x.dtype, x.device, stream, "state_out")
+    out = _new(out, (B, E), x.dtype, x.device, stream, "out")
+    status = lib.gtr_causal_conv_step(x.data_ptr(), _row_stride(x, "x"), state.data_ptr(), weight.data_ptr(), _ptr(bias),
+                                      int(bool(silu)), B, E, W, code, out.data_ptr(), new.data_ptr(), _stream_ptr(stream))
+    _check(status, "gtr_causal_conv_step", lib)
+    return out, new
+
+
+def _ssm_args(lead, x, delta, A, Bm, C, D, z, delta_bias):
+    E, N = x.shape[-1], A.shape[-1]
+    _on_device(x, x=x, delta=delta, A=A, Bm=Bm, C=C, D=D, z=z, delta_bias=delta_bias)
+    _like(A, torch.float32, (E, N), "A")
+    for name, t in (("D", D), ("delta_bias", delta_bias)):
+        if t is not None:
+            _like(t, torch.float32, (E,), name)
+    strides = []
+    for name, t, width in (("x", x, E), ("delta", delta, E), ("z", z, E), ("Bm", Bm, N), ("C", C, N)):
+        if t is None:
+            strides.append(0)
+            continue
+        if tuple(t.shape) != (*lead, width) or t.dtype != x.dtype:
+            raise ValueError(f"{name} must be {[*lead, width]} of x's dtype")
+        strides.append(_row_stride(t, name))
+    return E, N, strides
+
+
+def ssm_scan(x: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, Bm: torch.Tensor, C: torch.Tensor, grid_h: int,
+             grid_w: int, order: int = ROW_FWD, D: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None,
+             delta_bias: Optional[torch.Tensor] = None, softplus: bool = True,
+             initial_state: Optional[torch.Tensor] = None, final_state=True, out: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Selective state-space scan along a scan order through ``gtr_ssm_scan_fwd``.  x, delta, z: [B, T, E]; Bm, C:
+    [B, T, N]; one dtype, each with its own token stride; A: [E, N], D, delta_bias: [E], initial_state: [B, E, N],
+    float32.  ``final_state``: True (allocate), None/False (skip) or a [B, E, N] float32 tensor.  Returns
+    (out [B, T, E], final_state)."""
+    lib, code = load(), _code(x)
+    B, T, E = _sequence(x, grid_h, grid_w)
+    E, N, (xs, ds, zs, bs, cs) = _ssm_args((B, T), x, delta, A, Bm, C, D, z, delta_bias)
+    if initial_state is not None:
+        _on_device(x, initial_state=initial_state)
+        _like(initial_state, torch.float32, (B, E, N), "initial_state")
+    out = _new(out, (B, T, E), x.dtype, x.device, stream, "out")
+    fs = None
+    if final_state is not None and final_state is not False:
+        fs = _new(None if final_state is True else final_state, (B, E, N), torch.float32, x.device, stream, "final_state")
+    status = lib.gtr_ssm_scan_fwd(x.data_ptr(), xs, delta.data_ptr(), ds, A.data_ptr(), Bm.data_ptr(), bs, C.data_ptr(), cs,
+                                  _ptr(D), _ptr(z), zs, _ptr(delta_bias), int(bool(softplus)), _ptr(initial_state), B,
+                                  grid_h, grid_w, E, N, order, code, out.data_ptr(), _ptr(fs), _stream_ptr(stream))
+    _check(status, "gtr_ssm_scan_fwd", lib)
+    return out, fs
+
+
+def ssm_step(x: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, Bm: torch.Tensor, C: torch.Tensor,
+             state: torch.Tensor, D: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None,
+             delta_bias: Optional[torch.Tensor] = None, softplus: bool = True, state_out: Optional[torch.Tensor] = None,
+             out: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The next token of every sequence through ``gtr_ssm_step``.  x, delta, z: [B, E]; Bm, C: [B, N]; state: [B, E, N]
+    float32, updated in place unless ``state_out`` is given.  Returns (out [B, E], the new state)."""
+    lib, code = load(), _code(x)
+    if x.dim() != 2:
+        raise ValueError("x must be [B, E]")
+    B = x.shape[0]
+    E, N, (xs, ds, zs, bs, cs) = _ssm_args((B,), x, delta, A, Bm, C, D, z, delta_bias)
+    _on_device(x, state=state)
+    _like(state, torch.float32, (B, E, N), "state")
+    new = _new(state if state_out is None else state_out, state.shape, torch.float32, x.device, stream, "state_out")
+    out = _new(out, (B, E), x.dtype, x.device, stream, "out")
+    status = lib.gtr_ssm_step(x.data_ptr(), xs, delta.data_ptr(), ds, A.data_ptr(), Bm.data_ptr(), bs, C.data_ptr(), cs,
+                              _ptr(D), _ptr(z), zs, _ptr(delta_bias), int(bool(softplus)), state.data_ptr(), B, E, N, code,
+                              out.data_ptr(), new.data_ptr(), _stream_ptr(stream))
+    _check(status, "gtr_ssm_step", lib)
+    return out, new
+
+
+def _ffn_args(x, w_gate, w_value):
+    code = _code(x)
+    if x.dtype == torch.float32:
+        raise GLAError(2, "gtr_swiglu_ffn: float16 or bfloat16 only")
+    D, F = x.shape[-1], w_gate.shape[0]
+    _on_device(x, x=x, w_gate=w_gate, w_value=w_value)
+    _like(w_gate, x.dtype, (F, D), "w_gate")
+    _like(w_value, x.dtype, (F, D), "w_value")
+    return code, x.numel() // max(D, 1), D, F, _row_stride(x, "x")
+
+
+def swiglu_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_value: torch.Tensor, out: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Gated feed-forward step through ``gtr_swiglu_ffn_fwd``: SiLU(x w_gate^T) * (x w_value^T).  x: [..., D];
+    w_gate, w_value: [F, D]; one dtype, float16 or bfloat16; D and F multiples of 8.  Returns [..., F]."""
+    lib = load()
+    code, M, D, F, xs = _ffn_args(x, w_gate, w_value)
+    out = _new(out, (*x.shape[:-1], F), x.dtype, x.device, stream, "out")
+    status = lib.gtr_swiglu_ffn_fwd(x.data_ptr(), xs, w_gate.data_ptr(), w_value.data_ptr(), M, D, F, code, out.data_ptr(),
+                                    _stream_ptr(stream))
+    _check(status, "gtr_swiglu_ffn_fwd", lib)
+    return out
+
+
+def swiglu_ffn_backward_workspace_bytes(M: int, D: int, F: int) -> int:
+    """Device workspace ``swiglu_ffn_backward`` needs for M tokens."""
+    return int(load().gtr_swiglu_ffn_bwd_workspace_bytes(M, D, F))
+
+
+def swiglu_ffn_backward(dout: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_value: torch.Tensor,
+                        stream: Optional[torch.cuda.Stream] = None,
+                        workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Backward pass of :func:`swiglu_ffn` through ``gtr_swiglu_ffn_bwd``: (dx, dw_gate, dw_value) for the gradient
+    dout of its output, in the inputs' dtype.  ``workspace``: a CUDA uint8 tensor of at least
+    ``swiglu_ffn_backward_workspace_bytes()`` that no overlapping call shares."""
+    lib = load()
+    code, M, D, F, xs = _ffn_args(x, w_gate, w_value)
+    _on_device(x, dout=dout, workspace=workspace)
+    if tuple(dout.shape) != (*x.shape[:-1], F) or dout.dtype != x.dtype:
+        raise ValueError("dout must be [..., F] of x's leading shape and dtype")
+    dx = _new(None, x.shape, x.dtype, x.device, stream, "dx")
+    dwg = _new(None, (F, D), x.dtype, x.device, stream, "dw_gate")
+    dwv = _new(None, (F, D), x.dtype, x.device, stream, "dw_value")
+    if workspace is None:
+        workspace = _new(None, (swiglu_ffn_backward_workspace_bytes(M, D, F),), torch.uint8, x.device, stream, "workspace")
+    status = lib.gtr_swiglu_ffn_bwd(dout.data_ptr(), _row_stride(dout, "dout"), x.data_ptr(), xs, w_gate.data_ptr(),
+                                    w_value.data_ptr(), M, D, F, code, dx.data_ptr(), dwg.data_ptr(), dwv.data_ptr(),
+                                    workspace.data_ptr(), _nbytes(workspace), _stream_ptr(stream))
+    _check(status, "gtr_swiglu_ffn_bwd", lib)
+    return dx, dwg, dwv
 
 
 RAN = {0: "none", 1: "simt", 2: "tc", 3: "tc_split", 4: "tc_balanced"}
