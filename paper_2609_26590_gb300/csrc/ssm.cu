@@ -4,29 +4,36 @@
 // per channel, with N states a channel, A and D of the channel and B_s, C_s of the token.
 //
 // A decay of its own for every (channel, state) leaves nothing for the tensor cores: the work is one
-// power of two and four multiply-adds a token, channel and state on the CUDA cores.  LPC lanes share a
-// channel's states, NS each in packed fp32 pairs; a warp owns 32 / LPC channels and walks the
-// positions of its segment in blocks of 16: the lanes stage dt, dt x, B and C as fp32 in the warp's
-// shared memory (no barrier beyond the warp), then every lane steps its states.  The LPC partial
-// readouts of LPC tokens are exchanged at once so that each lane ends with the whole readout of the
-// token it loaded x and z of, and stores it.
+// power of two and four multiply-adds a token, channel and state on the CUDA cores.  A lane owns a channel and up to
+// 16 of its states in packed fp32 pairs (LPC lanes share a channel of more); a warp owns 32 / LPC channels and
+// one segment of the scan positions and needs no other warp while it walks: its rows arrive by cp.async a few
+// blocks of 8 positions ahead (the scan order is in their addresses), B and C are widened to fp32 once for all
+// its lanes, which read them by broadcast, and the outputs leave through shared memory in 16-byte pieces.
 //
-// Few channels leave SMs idle, so short launches cut the sequence into one segment a warp of the
-// CTA: a first walk yields each segment's end state from zero and its sum of dt (the segment's
-// decay is exp(A sum dt)), the CTA folds them in order, and the second walk starts from the fold.
+// Few channels leave schedulers idle or with a single warp whose dependent instructions nothing hides, so the
+// sequence is cut into a segment a warp, over the warps of a CTA and the CTAs of a thread-block cluster: a first
+// walk yields each segment's end state from zero and its sum of dt (the segment's decay is exp(A sum dt)), the
+// warps fold the earlier segments of their CTA and then the earlier CTAs' totals out of their shared memory, and
+// the second walk starts from the fold.
 #include <cuda_runtime.h>
+
+#include <mutex>
+#include <type_traits>
 
 #include "elem.cuh"
 #include "f32x2.cuh"
 #include "gla_internal.h"
 #include "scanpos.cuh"
+#include "tc_ptx.cuh"
 
 namespace gtr {
 namespace {
 
-constexpr int kSsmBlock = 16;     // positions staged at once
-constexpr int kSsmMaxWarps = 16;  // segments of a CTA
-constexpr int kSsmWarps = 4;      // channel groups of a CTA that does not split
+constexpr int kSsmBlock = 8;        // positions of a block
+constexpr int kSsmWarps = 4;        // warps of a CTA that does not split sequences
+constexpr int kSsmMaxWarps = 8;
+constexpr int kSsmMinCtas = 2;
+constexpr int kSsmMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct SsmParams {
@@ -37,8 +44,8 @@ struct SsmParams {
     float *state;
     ScanGrid grid;
     int B, E, N, softplus;
-    int groups;   // channel groups of a sequence
-    int nseg, seg_len;
+    int groups, units;           // channel groups of a sequence, and of all
+    int cluster, nseg, seg_len;  // CTAs of a cluster, segments of a sequence, positions of a segment
 };
 
 __device__ __forceinline__ float exp2_hw(float a) {
@@ -47,168 +54,415 @@ __device__ __forceinline__ float exp2_hw(float a) {
     return r;
 }
 
-// softplus(v) = max(v, 0) + log(1 + e^{-|v|}): log1p keeps the small steps of very negative v.
-__device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.f) + log1pf(__expf(-fabsf(v))); }
-
-// Sum over the LPC lanes of a channel of LPC values each: lane q ends with the sum of value q.
-template <int LPC> __device__ __forceinline__ float exchange_sum(float (&v)[LPC], int q) {
-#pragma unroll
-    for (int o = LPC / 2; o > 0; o >>= 1) {
-        const bool hi = q & o;
-#pragma unroll
-        for (int i = 0; i < o; ++i) {
-            const float keep = hi ? v[i + o] : v[i], send = hi ? v[i] : v[i + o];
-            v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
-        }
-    }
-    return v[0];
+// softplus(v) = max(v, 0) + log(1 + e^{-|v|}).  The logarithm keeps the small steps of very negative v:
+// log(1 + e) = 2 artanh(s) with s = e / (2 + e) <= 1/3, and artanh(s) / s is a polynomial in s^2 on [0, 1/9]
+// (minimax by Remez exchange, relative error 4e-9).  A NaN stays one.
+__device__ __forceinline__ float softplus(float v) {
+    const float e = exp2_hw(-fabsf(v) * kLog2e), s = __fdividef(e, 2.f + e), r = s * s;
+    float f = fmaf(r, 0.1408916763f, 0.1398030134f);
+    f = fmaf(r, f, 0.2001245514f);
+    f = fmaf(r, f, 0.3333315734f);
+    f = fmaf(r, f, 1.000000004f);
+    return fmaf(2.f * s, f, fmaxf(v, 0.f));
+}
+// on ? a : b without a branch: the tokens of a block stay one run of instructions that interleave.
+__device__ __forceinline__ float select(bool on, float a, float b) {
+    float r;
+    asm("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\tselp.f32 %0, %1, %2, p;\n\t}"
+        : "=f"(r)
+        : "f"(a), "f"(b), "r"(static_cast<uint32_t>(on)));
+    return r;
 }
 
-template <typename E, int LPC, int NS>
-__global__ void __launch_bounds__(kSsmMaxWarps * 32) ssm_kernel(const __grid_constant__ SsmParams p) {
-    constexpr int CH = 32 / LPC, NP = LPC * NS, TL = kSsmBlock / LPC, NB = kSsmBlock * NP / 32;
-    constexpr int kWarpFloats = kSsmBlock * (2 * CH + 2 * NP);
+template <int BYTES> __device__ __forceinline__ void cp_async(void *dst, const void *src, bool in) {  // zeros when !in
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(dst)), "l"(src), "r"(in ? 16 : 0)
+                     : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(ptx::smem_u32(dst)), "l"(src),
+                     "r"(in ? BYTES : 0), "n"(BYTES)
+                     : "memory");
+}
+template <int BYTES> struct Piece;
+template <> struct Piece<2> { using type = uint16_t; };
+template <> struct Piece<4> { using type = uint32_t; };
+template <> struct Piece<16> { using type = uint4; };
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// What a warp holds in shared memory, for CH channels and NP (padded) states.
+template <typename E, int CH, int NP> struct SsmWarp {
+    static constexpr bool kWiden = sizeof(E) == 2;
+    static constexpr int kStages = kWiden ? 4 : 3;  // blocks as they are stored
+    struct Raw {  // one block as it is stored
+        E x[kSsmBlock][CH], delta[kSsmBlock][CH], z[kSsmBlock][CH], b[kSsmBlock][NP], c[kSsmBlock][NP];
+    };
+    Raw raw[kStages];
+    // one block's B and C in fp32, and the next one's (fp32 elements are read where they are)
+    float b[kWiden ? 2 : 1][kWiden ? kSsmBlock : 1][NP], c[kWiden ? 2 : 1][kWiden ? kSsmBlock : 1][NP];
+    E out[kSsmBlock][CH];
+    // the segment's end state from zero and its sum of dt (state rows of CH channels)
+    float end[NP][CH], sum_dt[CH];
+};
+template <int CH, int NP> struct SsmTotal {  // the same of a CTA's segments
+    float end[NP][CH], sum_dt[CH];
+};
+
+// Four neighbouring elements as fp32.
+template <typename E> __device__ __forceinline__ float4 ld_quad(const E *p) {
+    const uint2 w = *reinterpret_cast<const uint2 *>(p);
+    const float2 a = unpack16<E>(w.x), b = unpack16<E>(w.y);
+    return make_float4(a.x, a.y, b.x, b.y);
+}
+template <> __device__ __forceinline__ float4 ld_quad<float>(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+
+template <typename E, int LPC, int NS, int W>
+__global__ void __launch_bounds__(32 * kSsmMaxWarps, kSsmMinCtas) ssm_kernel(const __grid_constant__ SsmParams p) {
+    constexpr int CH = 32 / LPC, NP = LPC * NS, H2 = NS / 2;
+    constexpr bool ASYNC = W * sizeof(E) >= 4;  // cp.async takes 4 or 16 bytes
+    using Warp = SsmWarp<E, CH, NP>;
+    constexpr int kStages = Warp::kStages;
     extern __shared__ float4 smem4[];
-    float *smem = reinterpret_cast<float *>(smem4);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ch = lane / LPC, q = lane % LPC;
-    const bool split = p.nseg > 1;
-    const long long unit = split ? blockIdx.x : (long long)blockIdx.x * kSsmWarps + warp;
-    if (unit >= (long long)p.B * p.groups) return;  // whole warps, and only where the CTA has no barrier
-    const int b = static_cast<int>(unit / p.groups), c = static_cast<int>(unit - (long long)b * p.groups) * CH + ch;
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, ch = lane % CH, q = lane / CH;
+    Warp &sm = reinterpret_cast<Warp *>(smem4)[w];
+    // a warp's unit (sequence and channel group) and segment
+    int unit, seg, rank = 0;
+    if (p.nseg > 1) {
+        rank = static_cast<int>(ptx::cluster_ctarank());
+        unit = static_cast<int>(blockIdx.x) / p.cluster;
+        seg = rank * warps + w;
+    } else {
+        unit = static_cast<int>(blockIdx.x) * warps + w;
+        seg = 0;
+        if (unit >= p.units) return;  // (no barrier below in this mode)
+    }
+    const int b = unit / p.groups, c0 = (unit - b * p.groups) * CH, c = c0 + ch;
     const bool live = c < p.E;
     const int T = p.grid.T;
-    const int seg = split ? warp : 0;
-    const int t0 = split ? (seg * p.seg_len < T ? seg * p.seg_len : T) : 0;
-    const int t1 = split ? (T - t0 < p.seg_len ? T : t0 + p.seg_len) : T;
-    float2 *s_dt = reinterpret_cast<float2 *>(smem + (size_t)warp * kWarpFloats);  // [block][CH]: dt, dt x
-    float *s_b = smem + (size_t)warp * kWarpFloats + 2 * kSsmBlock * CH;            // [block][NP]
-    float *s_c = s_b + kSsmBlock * NP;
+    const long long first = (long long)seg * p.seg_len;
+    const int t0 = first < T ? static_cast<int>(first) : T, t1 = T - t0 < p.seg_len ? T : t0 + p.seg_len;
+    const int nblk = (t1 - t0 + kSsmBlock - 1) / kSsmBlock;  // 0: an empty segment behind the sequence
     const long long seq = (long long)b * T;
-    const E *x = static_cast<const E *>(p.x) + seq * p.x_stride + (live ? c : 0);
-    const E *dl = static_cast<const E *>(p.delta) + seq * p.delta_stride + (live ? c : 0);
-    const E *z = p.z ? static_cast<const E *>(p.z) + seq * p.z_stride + (live ? c : 0) : nullptr;
+    const E *x = static_cast<const E *>(p.x) + seq * p.x_stride + c0;
+    const E *dl = static_cast<const E *>(p.delta) + seq * p.delta_stride + c0;
+    const E *z = p.z ? static_cast<const E *>(p.z) + seq * p.z_stride + c0 : nullptr;
     const E *Bm = static_cast<const E *>(p.Bm) + seq * p.b_stride;
     const E *C = static_cast<const E *>(p.C) + seq * p.c_stride;
-    E *out = static_cast<E *>(p.out) + seq * p.E + (live ? c : 0);
-    const float bias = p.bias && live ? p.bias[c] : 0.f, skip = p.D && live ? p.D[c] : 0.f;
-    f2 a2[NS / 2], h[NS / 2];
-#pragma unroll
-    for (int i = 0; i < NS / 2; ++i) {
-        float v[2], s[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int n = q * NS + 2 * i + k;
-            const bool in = live && n < p.N;
-            v[k] = in ? p.A[(long long)c * p.N + n] * kLog2e : 0.f;
-            s[k] = in && p.init ? p.init[((long long)b * p.E + c) * p.N + n] : 0.f;
-        }
-        a2[i] = pack2(v[0], v[1]);
-        h[i] = pack2(s[0], s[1]);
-    }
-    float sum_dt = 0.f;
+    E *out = static_cast<E *>(p.out) + seq * p.E + c0;
+    const float bias = live && p.bias ? p.bias[c] : 0.f, skip = live && p.D ? p.D[c] : 0.f;
 
-    auto walk = [&](bool readout) {
-        for (int s0 = t0; s0 < t1; s0 += kSsmBlock) {
-            float xv[TL], zv[TL];
-            int tok[TL];
-            __syncwarp();
+    f2 a2[H2], h[H2];
+    // a lane's states of a [E, N] row: 16-byte pieces where rows start on them
+    auto load_states = [&](f2(&v)[H2], const float *rows, long long row) {
+        const float *src = rows + row * p.N + q * NS;
 #pragma unroll
-            for (int j = 0; j < TL; ++j) {
-                const int s = s0 + j * LPC + q;
-                const bool in = live && s < t1;
-                ScanPos pos;
-                pos.set(p.grid, in ? s : t0);
-                tok[j] = pos.t;
-                float dt = 0.f;
-                xv[j] = zv[j] = 0.f;
-                if (in) {
-                    xv[j] = to_f32(x[pos.t * p.x_stride]);
-                    dt = to_f32(dl[pos.t * p.delta_stride]) + bias;
-                    if (p.softplus) dt = softplus(dt);
-                    if (readout && z) zv[j] = to_f32(z[pos.t * p.z_stride]);
+        for (int i = 0; i < H2; i += 2) {
+            float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+            const int n = q * NS + 2 * i;
+            if (live && n < p.N) {
+                if (p.N % 4 == 0) {
+                    f = *reinterpret_cast<const float4 *>(src + 2 * i);
+                } else {
+                    f.x = src[2 * i];
+                    if (n + 1 < p.N) f.y = src[2 * i + 1];
+                    if (n + 2 < p.N) f.z = src[2 * i + 2];
+                    if (n + 3 < p.N) f.w = src[2 * i + 3];
                 }
-                s_dt[(j * LPC + q) * CH + ch] = make_float2(dt, dt * xv[j]);
             }
+            v[i] = pack2(f.x, f.y);
+            v[i + 1] = pack2(f.z, f.w);
+        }
+    };
+    const long long state_row = (long long)b * p.E + c;
+    auto load_start = [&] {
+        if (p.init) {
+            load_states(h, p.init, state_row);
+        } else {
 #pragma unroll
-            for (int k = 0; k < NB; ++k) {
-                const int i = k * 32 + lane, s = s0 + i / NP, n = i % NP;
-                float vb = 0.f, vc = 0.f;
-                if (s < t1 && n < p.N) {
-                    ScanPos pos;
-                    pos.set(p.grid, s);
-                    vb = to_f32(Bm[pos.t * p.b_stride + n]);
-                    if (readout) vc = to_f32(C[pos.t * p.c_stride + n]);
-                }
-                s_b[i] = vb;
-                s_c[i] = vc;
+            for (int i = 0; i < H2; ++i) h[i] = 0;
+        }
+    };
+    load_states(a2, p.A, c);
+#pragma unroll
+    for (int i = 0; i < H2; ++i) a2[i] = mul2(a2[i], pack2(kLog2e, kLog2e));
+
+    // Loads of one block in pieces of W elements: rows of CH channels and of the states, from the tokens of its
+    // positions; zeros outside.  Single 16-bit elements, which cp.async does not copy, go through registers:
+    // `load` fetches them and `put` stores them a block's work later.
+    constexpr int XC = CH / W, BC = NP / W, PX = (kSsmBlock * XC + 31) / 32, PB = (kSsmBlock * BC + 31) / 32;
+    E rx[ASYNC ? 1 : PX], rd[ASYNC ? 1 : PX], rz[ASYNC ? 1 : PX], rb[ASYNC ? 1 : PB], rc[ASYNC ? 1 : PB];
+    auto load = [&](int blk, bool readout) {
+        typename Warp::Raw &r = sm.raw[blk % kStages];
+        const int s0 = t0 + blk * kSsmBlock;
+#pragma unroll
+        for (int k = 0; k < PX; ++k) {
+            const int i = 32 * k + lane, t = i / XC, e = (i % XC) * W, s = s0 + t;
+            if (kSsmBlock * XC % 32 != 0 && i >= kSsmBlock * XC) break;
+            const bool in = s < t1 && c0 + e < p.E;
+            ScanPos pos;
+            pos.set(p.grid, in ? s : t0);
+            const int o = in ? e : 0;
+            const E *px = x + pos.t * p.x_stride + o, *pd = dl + pos.t * p.delta_stride + o;
+            const E *pz = readout && p.z ? z + pos.t * p.z_stride + o : nullptr;
+            if constexpr (ASYNC) {
+                cp_async<W * sizeof(E)>(&r.x[t][e], px, in);
+                cp_async<W * sizeof(E)>(&r.delta[t][e], pd, in);
+                if (pz) cp_async<W * sizeof(E)>(&r.z[t][e], pz, in);
+            } else {
+                const E zero = from_f32<E>(0.f);
+                rx[k] = in ? *px : zero;
+                rd[k] = in ? *pd : zero;
+                rz[k] = in && pz ? *pz : zero;
             }
-            __syncwarp();
+        }
 #pragma unroll
-            for (int j = 0; j < TL; ++j) {
-                float part[LPC];
-#pragma unroll
-                for (int u = 0; u < LPC; ++u) {
-                    const int t = j * LPC + u;
-                    const float2 d = s_dt[t * CH + ch];
-                    const f2 dt2 = pack2(d.x, d.x), du2 = pack2(d.y, d.y);
-                    const f2 *bp = reinterpret_cast<const f2 *>(s_b + t * NP + q * NS);
-                    const f2 *cp = reinterpret_cast<const f2 *>(s_c + t * NP + q * NS);
-                    f2 acc = 0;
-                    sum_dt += d.x;
-#pragma unroll
-                    for (int i = 0; i < NS / 2; ++i) {
-                        const float2 e = unpack2(mul2(dt2, a2[i]));
-                        h[i] = fma2(pack2(exp2_hw(e.x), exp2_hw(e.y)), h[i], mul2(du2, bp[i]));
-                        acc = fma2(cp[i], h[i], acc);
-                    }
-                    const float2 r = unpack2(acc);
-                    part[u] = r.x + r.y;
-                }
-                if (readout) {
-                    float y = exchange_sum<LPC>(part, q);
-                    y = fmaf(skip, xv[j], y);
-                    if (z) y *= silu<E>(zv[j]);
-                    if (live && s0 + j * LPC + q < t1) out[(long long)tok[j] * p.E] = from_f32<E>(y);
-                }
+        for (int k = 0; k < PB; ++k) {
+            const int i = 32 * k + lane, t = i / BC, n = (i % BC) * W, s = s0 + t;
+            if (kSsmBlock * BC % 32 != 0 && i >= kSsmBlock * BC) break;
+            const bool in = s < t1 && n < p.N;
+            ScanPos pos;
+            pos.set(p.grid, in ? s : t0);
+            const int o = in ? n : 0;
+            const E *pb = Bm + pos.t * p.b_stride + o, *pc = C + pos.t * p.c_stride + o;
+            if constexpr (ASYNC) {
+                cp_async<W * sizeof(E)>(&r.b[t][n], pb, in);
+                if (readout) cp_async<W * sizeof(E)>(&r.c[t][n], pc, in);
+            } else {
+                const E zero = from_f32<E>(0.f);
+                rb[k] = in ? *pb : zero;
+                rc[k] = in && readout ? *pc : zero;
             }
         }
     };
-
-    if (split) {
-        float *sum_h = smem + (size_t)p.nseg * kWarpFloats;  // [nseg][CH][NP]
-        float *sum_d = sum_h + (size_t)p.nseg * CH * NP;     // [nseg][CH]
-        f2 start[NS / 2];
+    auto put = [&](int blk) {
+        if constexpr (!ASYNC) {
+            typename Warp::Raw &r = sm.raw[blk % kStages];
 #pragma unroll
-        for (int i = 0; i < NS / 2; ++i) start[i] = h[i], h[i] = 0;
-        if (seg + 1 < p.nseg) {  // nothing follows the last segment
-            walk(false);
+            for (int k = 0; k < PX; ++k) {
+                const int i = 32 * k + lane, t = i / XC, e = i % XC;
+                if (kSsmBlock * XC % 32 != 0 && i >= kSsmBlock * XC) break;
+                r.x[t][e] = rx[k], r.delta[t][e] = rd[k], r.z[t][e] = rz[k];
+            }
 #pragma unroll
-            for (int i = 0; i < NS / 2; ++i)
-                reinterpret_cast<f2 *>(sum_h + ((size_t)seg * CH + ch) * NP + q * NS)[i] = h[i];
-            if (q == 0) sum_d[seg * CH + ch] = sum_dt;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < NS / 2; ++i) h[i] = start[i];
-        for (int j = 0; j < seg; ++j) {
-            const float d = sum_d[j * CH + ch];
-            const f2 *e = reinterpret_cast<const f2 *>(sum_h + ((size_t)j * CH + ch) * NP + q * NS);
-#pragma unroll
-            for (int i = 0; i < NS / 2; ++i) {
-                const float2 m = unpack2(mul2(pack2(d, d), a2[i]));
-                h[i] = fma2(pack2(exp2_hw(m.x), exp2_hw(m.y)), h[i], e[i]);
+            for (int k = 0; k < PB; ++k) {
+                const int i = 32 * k + lane, t = i / BC, n = i % BC;
+                if (kSsmBlock * BC % 32 != 0 && i >= kSsmBlock * BC) break;
+                r.b[t][n] = rb[k], r.c[t][n] = rc[k];
             }
         }
-    }
-    walk(true);
-    if (p.state && live && seg + 1 == p.nseg) {
+    };
+    auto widen = [&](int blk, bool readout) {
+        if (!Warp::kWiden) return;
+        const typename Warp::Raw &r = sm.raw[blk % kStages];
 #pragma unroll
-        for (int i = 0; i < NS / 2; ++i) {
-            const float2 v = unpack2(h[i]);
-            float *dst = p.state + ((long long)b * p.E + c) * p.N;
+        for (int i = lane; i < kSsmBlock * NP / 4; i += 32) {
+            const int t = i / (NP / 4), n = 4 * (i % (NP / 4));
+            *reinterpret_cast<float4 *>(&sm.b[blk & 1][t][n]) = ld_quad<E>(&r.b[t][n]);
+            if (readout) *reinterpret_cast<float4 *>(&sm.c[blk & 1][t][n]) = ld_quad<E>(&r.c[t][n]);
+        }
+    };
+    float sum_dt = 0.f;
+    const bool soft = p.softplus, gated = p.z != nullptr;
+    // One token: the states' step and, with readout, its output.
+    auto token = [&](const typename Warp::Raw &r, int buf, int t, bool readout) {
+        const float xv = to_f32(r.x[t][ch]), v = to_f32(r.delta[t][ch]) + bias;
+        const float dt = select(soft, softplus(v), v);
+        const f2 dt2 = pack2(dt, dt), du2 = pack2(dt * xv, dt * xv);
+        const ulonglong2 *bp = reinterpret_cast<const ulonglong2 *>(
+            Warp::kWiden ? &sm.b[buf][t][q * NS] : reinterpret_cast<const float *>(&r.b[t][q * NS]));
+        const ulonglong2 *cp = reinterpret_cast<const ulonglong2 *>(
+            Warp::kWiden ? &sm.c[buf][t][q * NS] : reinterpret_cast<const float *>(&r.c[t][q * NS]));
+        f2 acc[2] = {pack2(q == 0 ? skip * xv : 0.f, 0.f), 0};
+        if (!readout) sum_dt += dt;
+#pragma unroll
+        for (int i = 0; i < H2; i += 2) {
+            const ulonglong2 bv = bp[i / 2];
+            const float2 e0 = unpack2(mul2(dt2, a2[i])), e1 = unpack2(mul2(dt2, a2[i + 1]));
+            h[i] = fma2(pack2(exp2_hw(e0.x), exp2_hw(e0.y)), h[i], mul2(du2, bv.x));
+            h[i + 1] = fma2(pack2(exp2_hw(e1.x), exp2_hw(e1.y)), h[i + 1], mul2(du2, bv.y));
+            if (readout) {
+                const ulonglong2 cv = cp[i / 2];
+                acc[0] = fma2(cv.x, h[i], acc[0]);
+                acc[1] = i == 0 ? mul2(cv.y, h[i + 1]) : fma2(cv.y, h[i + 1], acc[1]);
+            }
+        }
+        if (!readout) return 0.f;
+        const float2 s = unpack2(add2(acc[0], acc[1]));
+        float y = s.x + s.y;
+#pragma unroll
+        for (int o = CH; o < 32; o <<= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
+        return y * select(gated, silu<E>(to_f32(r.z[t][ch])), 1.f);
+    };
+    auto step = [&](int blk, bool readout) {
+        const typename Warp::Raw &r = sm.raw[blk % kStages];
+        const int left = t1 - t0 - blk * kSsmBlock;
+        if (left >= kSsmBlock) {
+            float y[kSsmBlock];  // no store between the tokens' loads
+#pragma unroll
+            for (int t = 0; t < kSsmBlock; ++t) y[t] = token(r, blk & 1, t, readout);
+            if (readout && q == 0) {
+#pragma unroll
+                for (int t = 0; t < kSsmBlock; ++t) sm.out[t][ch] = from_f32<E>(y[t]);
+            }
+        } else {
+#pragma unroll 1
+            for (int t = 0; t < left; ++t) {
+                const float y = token(r, blk & 1, t, readout);
+                if (readout && q == 0) sm.out[t][ch] = from_f32<E>(y);
+            }
+        }
+    };
+    auto store = [&](int blk) {
+        const int s0 = t0 + blk * kSsmBlock;
+        using R = typename Piece<W * sizeof(E)>::type;
+#pragma unroll
+        for (int i = lane; i < kSsmBlock * XC; i += 32) {
+            const int t = i / XC, e = (i % XC) * W, s = s0 + t;
+            if (s < t1 && c0 + e < p.E) {
+                ScanPos pos;
+                pos.set(p.grid, s);
+                *reinterpret_cast<R *>(out + (long long)pos.t * p.E + e) = *reinterpret_cast<const R *>(&sm.out[t][e]);
+            }
+        }
+    };
+    // The loads run kStages - 1 blocks ahead of the block that is stepped, the widening one block.
+    auto begin = [&](bool readout) {
+        __syncwarp();
+#pragma unroll 1
+        for (int i = 0; i < kStages - 1; ++i) {
+            if (i < nblk) {
+                load(i, readout);
+                put(i);
+            }
+            cp_async_commit();
+        }
+    };
+    auto walk = [&](auto readout_c) {
+        constexpr bool readout = decltype(readout_c)::value;
+        if (nblk == 0) return;
+        cp_async_wait<kStages - 2>();
+        __syncwarp();
+        widen(0, readout);
+#pragma unroll 1
+        for (int i = 0; i < nblk; ++i) {
+            cp_async_wait<kStages - 3>();
+            __syncwarp();  // block i + 1 has arrived, block i is widened, block i - 1 and its outputs are read
+            if (i + kStages - 1 < nblk) load(i + kStages - 1, readout);
+            cp_async_commit();
+            if (i + 1 < nblk) widen(i + 1, readout);
+            step(i, readout);
+            if (readout) {
+                __syncwarp();
+                store(i);
+            }
+            if (i + kStages - 1 < nblk) put(i + kStages - 1);
+        }
+        cp_async_wait<0>();
+    };
+
+    if (p.nseg == 1) {
+        begin(true);
+        load_start();
+    } else {
+        using Total = SsmTotal<CH, NP>;
+        Total &total = *reinterpret_cast<Total *>(reinterpret_cast<Warp *>(smem4) + warps);
+        // decay of a stretch whose dt sum to d, applied to v, plus its end state e
+        auto fold = [&](f2(&v)[H2], float d, const f2(&e)[H2]) {
+#pragma unroll
+            for (int i = 0; i < H2; ++i) {
+                const float2 m = unpack2(mul2(pack2(d, d), a2[i]));
+                v[i] = fma2(pack2(exp2_hw(m.x), exp2_hw(m.y)), v[i], e[i]);
+            }
+        };
+        auto put = [&](float (&end)[NP][CH], const f2(&v)[H2]) {
+#pragma unroll
+            for (int i = 0; i < H2; ++i) {
+                const float2 f = unpack2(v[i]);
+                end[q * NS + 2 * i][ch] = f.x;
+                end[q * NS + 2 * i + 1][ch] = f.y;
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < H2; ++i) h[i] = 0;
+        if (seg + 1 < p.nseg) {  // nothing follows the last segment
+            begin(false);
+            walk(std::false_type());
+        }
+        begin(true);  // the second walk's first blocks arrive while the segments are folded
+        put(sm.end, h);
+        if (q == 0) sm.sum_dt[ch] = sum_dt;
+        __syncthreads();
+        f2 pre[H2];  // the CTA's segments before this one, from zero
+#pragma unroll
+        for (int i = 0; i < H2; ++i) pre[i] = 0;
+        float pre_dt = 0.f;
+        auto fold_warp = [&](int j) {
+            const Warp &o = reinterpret_cast<const Warp *>(smem4)[j];
+            f2 e[H2];
+#pragma unroll
+            for (int i = 0; i < H2; ++i) e[i] = pack2(o.end[q * NS + 2 * i][ch], o.end[q * NS + 2 * i + 1][ch]);
+            fold(pre, o.sum_dt[ch], e);
+            pre_dt += o.sum_dt[ch];
+        };
+        for (int j = 0; j < w; ++j) fold_warp(j);
+        if (p.cluster > 1 && w + 1 == warps) {  // the CTA's total: with this warp's own end state, still in h
+            f2 t[H2];
+#pragma unroll
+            for (int i = 0; i < H2; ++i) t[i] = pre[i];
+            fold(t, sum_dt, h);
+            put(total.end, t);
+            if (q == 0) total.sum_dt[ch] = pre_dt + sum_dt;
+        }
+        load_start();
+        if (p.cluster > 1) {
+            __syncwarp();
+            ptx::cluster_sync();
+            float next_d = 0.f;
+            f2 next[H2];
+            auto get = [&](int j) {  // the total of CTA j
+                asm volatile("ld.shared::cluster.f32 %0, [%1];"
+                             : "=f"(next_d)
+                             : "r"(ptx::map_to_cta(ptx::smem_u32(&total.sum_dt[ch]), j)));
+                const uint32_t at = ptx::map_to_cta(ptx::smem_u32(&total.end[q * NS][ch]), j);
+#pragma unroll
+                for (int i = 0; i < H2; ++i) {
+                    float lo, hi;
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(lo) : "r"(at + 4 * CH * (2 * i)));
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(hi) : "r"(at + 4 * CH * (2 * i + 1)));
+                    next[i] = pack2(lo, hi);
+                }
+            };
+            if (rank > 0) get(0);
+            for (int j = 0; j < rank; ++j) {
+                const float d = next_d;
+                f2 e[H2];
+#pragma unroll
+                for (int i = 0; i < H2; ++i) e[i] = next[i];
+                if (j + 1 < rank) get(j + 1);
+                fold(h, d, e);
+            }
+            ptx::cluster_sync();  // every total is read: the CTAs may leave
+        }
+        fold(h, pre_dt, pre);
+    }
+    walk(std::true_type());
+    if (p.state && live && seg + 1 == p.nseg) {
+        float *dst = p.state + state_row * p.N + q * NS;
+#pragma unroll
+        for (int i = 0; i < H2; i += 2) {
+            const float2 lo = unpack2(h[i]), hi = unpack2(h[i + 1]);
             const int n = q * NS + 2 * i;
-            if (n < p.N) dst[n] = v.x;
-            if (n + 1 < p.N) dst[n + 1] = v.y;
+            if (n >= p.N) break;
+            if (p.N % 4 == 0) {
+                *reinterpret_cast<float4 *>(dst + 2 * i) = make_float4(lo.x, lo.y, hi.x, hi.y);
+            } else {
+                dst[2 * i] = lo.x;
+                if (n + 1 < p.N) dst[2 * i + 1] = lo.y;
+                if (n + 2 < p.N) dst[2 * i + 2] = hi.x;
+                if (n + 3 < p.N) dst[2 * i + 3] = hi.y;
+            }
         }
     }
 }
@@ -279,38 +533,131 @@ SsmParams ssm_params(const SsmProblem &q) {
     p.out = q.out, p.state = q.state_out;
     p.grid = make_scan_grid(q.grid_h, q.grid_w, q.order);
     p.B = q.B, p.E = q.E, p.N = q.N, p.softplus = q.softplus;
-    p.groups = p.nseg = p.seg_len = 0;
+    p.groups = p.units = p.cluster = p.nseg = p.seg_len = 0;
     return p;
 }
 
-template <typename E, int LPC, int NS> cudaError_t ssm_run(SsmParams &p, int n_sm, cudaStream_t stream) {
-    constexpr int CH = 32 / LPC, NP = LPC * NS;
-    constexpr int kWarpFloats = kSsmBlock * (2 * CH + 2 * NP);
-    p.groups = (p.E + CH - 1) / CH;
-    const long long units = (long long)p.B * p.groups;
-    // split while the warps would not fill the SMs' schedulers twice, at least two blocks a segment
-    const int blocks = (p.grid.T - 1) / kSsmBlock + 1;
-    int cap = kSsmMaxWarps;
-    while ((size_t)cap * (kWarpFloats + CH * NP + CH) * sizeof(float) > 48 * 1024) cap /= 2;
-    long long want = 8LL * n_sm / units;
-    if (want > cap) want = cap;
-    if (want > blocks / 2) want = blocks / 2;
-    p.nseg = want < 2 ? 1 : static_cast<int>(want);
-    const int per = (blocks + p.nseg - 1) / p.nseg;
-    p.nseg = (blocks + per - 1) / per;  // no empty segment
-    p.seg_len = per * kSsmBlock;
-    const int warps = p.nseg > 1 ? p.nseg : kSsmWarps;
-    const long long ctas = p.nseg > 1 ? units : (units + kSsmWarps - 1) / kSsmWarps;
-    if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
-    const size_t smem = (size_t)warps * (kWarpFloats + (p.nseg > 1 ? CH * NP + CH : 0)) * sizeof(float);
-    ssm_kernel<E, LPC, NS><<<static_cast<unsigned>(ctas), warps * 32, smem, stream>>>(p);
-    return cudaGetLastError();
+// How a launch cuts its sequences: segments over the warps of a CTA and the CTAs of a cluster.
+struct SsmPlan {
+    int warps, cluster, nseg, seg_len;
+};
+// The device's limits for one kernel, asked once: clusters of c CTAs of w warps that run at a time.
+struct SsmFit {
+    int sm = 0, active[2][kSsmMaxCluster + 1] = {};  // [w / 4 - 1][c]; [0][0]: CTAs that do not split
+};
+
+// The cheapest cut by what a launch takes: its clusters in waves of those the device places, a token kIssue[r]
+// cycles an instruction with r warps on a scheduler (warps take turns, one alone waits for its own results; measured
+// on a GB300 at 20 to 10,000 positions and 12 to 2,048 channel groups), two walks of 205 instructions a token and 16 states
+// against one of 115, and the start, the folds and the cluster's barriers beside them.
+SsmPlan ssm_plan(long long units, int T, const SsmFit &fit) {
+    static const float kIssue[5] = {0.f, 2.25f, 2.95f, 4.2f, 5.5f};
+    const int blocks = (T - 1) / kSsmBlock + 1;
+    SsmPlan best{kSsmWarps, 1, 1, T};
+    float least = 0.f;
+    for (int w = 4; w <= kSsmMaxWarps; w += 4)
+        for (int c = w == 4 ? 0 : 1; c <= kSsmMaxCluster; ++c) {
+            const int active = fit.active[w / 4 - 1][c], nseg = c == 0 ? 1 : w * c, per = (blocks + nseg - 1) / nseg;
+            if (c > 0 && (active < 1 || per < 2)) continue;
+            const long long n = c == 0 ? (units + w - 1) / w : units;
+            auto rate = [&](long long clusters) {  // of the busiest SM
+                const long long r = (clusters * (c == 0 ? 1 : c) + fit.sm - 1) / fit.sm * w / 4;
+                return kIssue[r < 4 ? r : 4];
+            };
+            float t = static_cast<float>(n / active) * rate(active) + rate(n % active);
+            t = t * per * kSsmBlock * (c == 0 ? 115.f : 205.f) + 6000.f * ((n + active - 1) / active);
+            if (c > 0) t += 300.f * w + 600.f * c + (c > 1 ? 2000.f : 0.f);
+            if (c == 0 || t < least) least = t, best = SsmPlan{w, c == 0 ? 1 : c, nseg, c == 0 ? T : per * kSsmBlock};
+        }
+    return best;
 }
-template <typename E> cudaError_t ssm_run_n(SsmParams &p, int n_sm, cudaStream_t s) {
-    if (p.N <= 8) return ssm_run<E, 2, 4>(p, n_sm, s);
-    if (p.N <= 16) return ssm_run<E, 4, 4>(p, n_sm, s);
-    if (p.N <= 32) return ssm_run<E, 8, 4>(p, n_sm, s);
-    return ssm_run<E, 8, 8>(p, n_sm, s);
+
+template <typename E, int LPC, int NS, int W> struct SsmLaunch {
+    static constexpr int CH = 32 / LPC, NP = LPC * NS;
+    static constexpr size_t kPerWarp = sizeof(SsmWarp<E, CH, NP>), kExtra = sizeof(SsmTotal<CH, NP>);
+
+    static size_t smem(int warps) { return warps * kPerWarp + kExtra; }
+    static void config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute &at, int warps, int cluster, unsigned ctas,
+                       cudaStream_t stream) {
+        cfg = {};
+        cfg.gridDim = dim3(ctas);
+        cfg.blockDim = dim3(32 * warps);
+        cfg.dynamicSmemBytes = smem(warps);
+        cfg.stream = stream;
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim.x = static_cast<unsigned>(cluster);
+        at.val.clusterDim.y = at.val.clusterDim.z = 1;
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+    }
+    // The device's limits, asked on the first launch on each device.
+    static cudaError_t fit(SsmFit *out) {
+        static std::mutex mutex;
+        static SsmFit known[64];
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        std::lock_guard<std::mutex> lock(mutex);
+        SsmFit &f = known[dev & 63];
+        if (f.sm == 0) {
+            auto *kernel = ssm_kernel<E, LPC, NS, W>;
+            SsmFit g;
+            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+            for (int w = 4; w <= kSsmMaxWarps && e == cudaSuccess; w += 4)
+                for (int c = 1; c <= kSsmMaxCluster && e == cudaSuccess && smem(w) <= 227 * 1024; ++c) {
+                    cudaLaunchConfig_t cfg;
+                    cudaLaunchAttribute at;
+                    config(cfg, at, w, c, c, nullptr);
+                    e = cudaOccupancyMaxActiveClusters(&g.active[w / 4 - 1][c], kernel, &cfg);
+                }
+            if (e != cudaSuccess) return e;
+            g.active[0][0] = g.active[0][1];
+            if (g.active[0][0] < 1) return cudaErrorInvalidConfiguration;
+            if ((e = sm_count(&g.sm)) != cudaSuccess) return e;
+            f = g;
+        }
+        *out = f;
+        return cudaSuccess;
+    }
+    static cudaError_t run(SsmParams &p, cudaStream_t stream) {
+        SsmFit f;
+        cudaError_t e = fit(&f);
+        if (e != cudaSuccess) return e;
+        p.groups = (p.E + CH - 1) / CH;
+        const long long units = (long long)p.B * p.groups;
+        if (units > (1 << 27)) return cudaErrorInvalidValue;  // 8 CTAs each
+        p.units = static_cast<int>(units);
+        const SsmPlan s = ssm_plan(units, p.grid.T, f);
+        p.cluster = s.cluster;
+        p.nseg = s.nseg;
+        p.seg_len = s.seg_len;
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute at;
+        config(cfg, at, s.warps, s.cluster,
+               static_cast<unsigned>(s.nseg > 1 ? units * s.cluster : (units + s.warps - 1) / s.warps), stream);
+        return cudaLaunchKernelEx(&cfg, ssm_kernel<E, LPC, NS, W>, p);
+    }
+};
+template <typename E, int W> cudaError_t ssm_run_n(SsmParams &p, cudaStream_t s) {
+    if (p.N <= 8) return SsmLaunch<E, 1, 8, W>::run(p, s);
+    if (p.N <= 16) return SsmLaunch<E, 1, 16, W>::run(p, s);
+    if (p.N <= 32) return SsmLaunch<E, 2, 16, W>::run(p, s);
+    return SsmLaunch<E, 4, 16, W>::run(p, s);
+}
+// The widest pieces that every row starts and ends on: 16 bytes, 4, or (16-bit elements) one.
+template <typename E> cudaError_t ssm_run(SsmParams &p, cudaStream_t s) {
+    constexpr int es = static_cast<int>(sizeof(E));
+    auto fits = [&](int bytes) {
+        const int v = bytes / es;
+        auto ok = [&](const void *q, long long stride) {
+            return reinterpret_cast<uintptr_t>(q) % bytes == 0 && stride % v == 0;
+        };
+        return p.E % v == 0 && p.N % v == 0 && ok(p.x, p.x_stride) && ok(p.delta, p.delta_stride) &&
+               (!p.z || ok(p.z, p.z_stride)) && ok(p.Bm, p.b_stride) && ok(p.C, p.c_stride);
+    };
+    if (fits(16)) return ssm_run_n<E, 16 / es>(p, s);
+    if (fits(4)) return ssm_run_n<E, 4 / es>(p, s);
+    return ssm_run_n<E, 1>(p, s);
 }
 
 template <typename E> cudaError_t ssm_step_e(SsmParams &p, cudaStream_t s) {
@@ -332,13 +679,10 @@ template <typename E> cudaError_t ssm_step_e(SsmParams &p, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_ssm(const SsmProblem &q, cudaStream_t stream) {
-    int n_sm = 0;
-    const cudaError_t e = sm_count(&n_sm);
-    if (e != cudaSuccess) return e;
     SsmParams p = ssm_params(q);
-    if (q.dtype == 0) return ssm_run_n<float>(p, n_sm, stream);
-    if (q.dtype == 1) return ssm_run_n<__half>(p, n_sm, stream);
-    return ssm_run_n<__nv_bfloat16>(p, n_sm, stream);
+    if (q.dtype == 0) return ssm_run<float>(p, stream);
+    if (q.dtype == 1) return ssm_run<__half>(p, stream);
+    return ssm_run<__nv_bfloat16>(p, stream);
 }
 
 cudaError_t launch_ssm_step(const SsmProblem &q, cudaStream_t stream) {
