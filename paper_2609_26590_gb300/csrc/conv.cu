@@ -4,8 +4,8 @@
 // the state from which single tokens go on.
 //
 // Memory-bound: each input is read once (and W - 1 again at the start of a strip, from L2), each
-// output written once.  A thread owns a 16-byte vector of channels (one channel where the
-// alignment does not allow vectors) and walks a strip of scan positions with the last W inputs
+// output written once.  A thread owns four channels (two or one where the
+// alignment does not allow that) and walks a strip of scan positions with the last W inputs
 // in registers; the scan order is in the walk's addresses.
 #include <cuda_runtime.h>
 
@@ -17,8 +17,8 @@ namespace gtr {
 namespace {
 
 constexpr int kConvThreads = 256;
-constexpr int kConvStrip = 16;  // scan positions a thread walks
-constexpr int kConvBatch = 4;   // loads in flight
+constexpr int kConvStrip = 32;  // most scan positions a thread walks
+constexpr int kConvBatch = 8;   // loads in flight
 
 struct ConvParams {
     const void *x;
@@ -27,52 +27,74 @@ struct ConvParams {
     const void *init;
     void *out, *state;
     ScanGrid grid;
-    int B, E, silu, strips;
+    int B, E, silu, strip, strips;  // positions of a strip, strips of a sequence
     long long items;  // B * strips
 };
 
+// The taps of VEC channels: VEC W consecutive floats, in 16-byte loads where they start on such.
+template <int VEC, int W> __device__ __forceinline__ void load_taps(const float *w, float (&tap)[W][VEC]) {
+    if (VEC * W % 4 == 0 && (reinterpret_cast<uintptr_t>(w) & 15u) == 0) {
+#pragma unroll
+        for (int i = 0; i < VEC * W / 4; ++i) {
+            const float4 f = reinterpret_cast<const float4 *>(w)[i];
+            const float v[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) tap[(4 * i + k) % W][(4 * i + k) / W] = v[k];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+#pragma unroll
+            for (int j = 0; j < W; ++j) tap[j][i] = w[i * W + j];
+    }
+}
+
 template <typename E, int VEC, int W>
-__global__ void __launch_bounds__(kConvThreads) conv_kernel(const __grid_constant__ ConvParams p) {
+__global__ void __launch_bounds__(kConvThreads, 2) conv_kernel(const __grid_constant__ ConvParams p) {
+    using Raw = typename Vec<E, VEC>::raw;
     const long long item = (long long)blockIdx.x * blockDim.y + threadIdx.y;
     const int c = (blockIdx.y * blockDim.x + threadIdx.x) * VEC;
     if (item >= p.items || c >= p.E) return;
     const int b = static_cast<int>(item / p.strips), strip = static_cast<int>(item - (long long)b * p.strips);
-    const int T = p.grid.T, s0 = strip * kConvStrip, s1 = T - s0 < kConvStrip ? T : s0 + kConvStrip;
+    const int T = p.grid.T, s0 = strip * p.strip, s1 = T - s0 < p.strip ? T : s0 + p.strip;
     const E *x = static_cast<const E *>(p.x) + (long long)b * T * p.x_stride + c;
     const E *init = p.init ? static_cast<const E *>(p.init) + (long long)b * (W - 1) * p.E + c : nullptr;
     E *out = static_cast<E *>(p.out) + (long long)b * T * p.E + c;
+    Raw in[kConvBatch];
+    ScanPos ahead, pos;
+    ahead.set(p.grid, s0);
+    pos = ahead;
+    auto fetch = [&](int s) {
+#pragma unroll
+        for (int k = 0; k < kConvBatch; ++k)
+            if (s + k < s1) {
+                in[k] = *reinterpret_cast<const Raw *>(x + (long long)ahead.t * p.x_stride);
+                ahead.next(p.grid);
+            }
+    };
+    fetch(s0);
     float w[W][VEC], bias[VEC], win[W][VEC];  // win: inputs s - W + 1 .. s
+    load_taps<VEC, W>(p.w + (long long)c * W, w);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        bias[i] = p.b ? p.b[c + i] : 0.f;
-#pragma unroll
-        for (int j = 0; j < W; ++j) w[j][i] = p.w[(long long)(c + i) * W + j];
-    }
-    ScanPos pos;
+    for (int i = 0; i < VEC; ++i) bias[i] = p.b ? p.b[c + i] : 0.f;
 #pragma unroll
     for (int j = 1; j < W; ++j) {  // inputs s0 - W + j
         const int s = s0 - W + j;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) win[j][i] = 0.f;
         if (s >= 0) {
-            pos.set(p.grid, s);
-            Vec<E, VEC>::unpack(ld_vec<E, VEC>(x + (long long)pos.t * p.x_stride), win[j]);
+            ScanPos q;
+            q.set(p.grid, s);
+            Vec<E, VEC>::unpack(ld_vec<E, VEC>(x + (long long)q.t * p.x_stride), win[j]);
         } else if (init) {
             Vec<E, VEC>::unpack(ld_vec<E, VEC>(init + (long long)(s + W - 1) * p.E), win[j]);
         }
     }
-    pos.set(p.grid, s0);
     for (int s = s0; s < s1; s += kConvBatch) {
-        typename Vec<E, VEC>::raw in[kConvBatch];
-        int tok[kConvBatch];
+        Raw now[kConvBatch];
 #pragma unroll
-        for (int k = 0; k < kConvBatch; ++k) {
-            tok[k] = pos.t;
-            if (s + k < s1) {
-                in[k] = *reinterpret_cast<const typename Vec<E, VEC>::raw *>(x + (long long)pos.t * p.x_stride);
-                pos.next(p.grid);
-            }
-        }
+        for (int k = 0; k < kConvBatch; ++k) now[k] = in[k];
+        fetch(s + kConvBatch);
 #pragma unroll
         for (int k = 0; k < kConvBatch; ++k) {
             if (s + k >= s1) break;
@@ -80,7 +102,7 @@ __global__ void __launch_bounds__(kConvThreads) conv_kernel(const __grid_constan
             for (int j = 0; j + 1 < W; ++j)
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) win[j][i] = win[j + 1][i];
-            Vec<E, VEC>::unpack(in[k], win[W - 1]);
+            Vec<E, VEC>::unpack(now[k], win[W - 1]);
             float a[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
@@ -89,7 +111,8 @@ __global__ void __launch_bounds__(kConvThreads) conv_kernel(const __grid_constan
                 for (int j = 0; j < W; ++j) a[i] = fmaf(w[j][i], win[j][i], a[i]);
                 if (p.silu) a[i] = silu<E>(a[i]);
             }
-            st_vec<E, VEC>(out + (long long)tok[k] * p.E, a);
+            st_vec<E, VEC>(out + (long long)pos.t * p.E, a);
+            pos.next(p.grid);
         }
     }
     if (p.state && s1 == T) {  // the window's last W - 1 inputs (exact: they are stored values)
@@ -111,7 +134,8 @@ __global__ void __launch_bounds__(kConvThreads) conv_step_kernel(const __grid_co
 #pragma unroll
     for (int j = 0; j + 1 < W; ++j) in[j] = ld_vec<E, VEC>(init + (long long)j * p.E);
     in[W - 1] = ld_vec<E, VEC>(static_cast<const E *>(p.x) + (long long)b * p.x_stride + c);
-    float a[VEC];
+    float a[VEC], w[W][VEC];
+    load_taps<VEC, W>(p.w + (long long)c * W, w);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) a[i] = p.b ? p.b[c + i] : 0.f;
 #pragma unroll
@@ -119,7 +143,7 @@ __global__ void __launch_bounds__(kConvThreads) conv_step_kernel(const __grid_co
         float f[VEC];
         Vec<E, VEC>::unpack(in[j], f);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) a[i] = fmaf(p.w[(long long)(c + i) * W + j], f[i], a[i]);
+        for (int i = 0; i < VEC; ++i) a[i] = fmaf(w[j][i], f[i], a[i]);
     }
     if (p.silu) {
 #pragma unroll
@@ -132,10 +156,15 @@ __global__ void __launch_bounds__(kConvThreads) conv_step_kernel(const __grid_co
         *reinterpret_cast<typename Vec<E, VEC>::raw *>(st + (long long)j * p.E) = in[j + 1];
 }
 
-template <typename E, int VEC, int W> cudaError_t conv_run(ConvParams &p, bool step, cudaStream_t stream) {
+template <typename E, int VEC, int W> cudaError_t conv_run(ConvParams &p, bool step, int n_sm, cudaStream_t stream) {
     const int nv = (p.E + VEC - 1) / VEC;
-    int ny = (nv + kConvThreads - 1) / kConvThreads;
+    const int ny = (nv + kConvThreads - 1) / kConvThreads;
     const int bx = (nv + ny - 1) / ny, by = kConvThreads / bx;  // bx <= 256
+    // strips as long as they still leave the SMs twice their threads
+    p.strip = kConvStrip;
+    while (p.strip > kConvBatch && (long long)p.B * ((p.grid.T - 1) / p.strip + 1) * nv < 1024LL * n_sm) p.strip /= 2;
+    p.strips = (p.grid.T - 1) / p.strip + 1;
+    p.items = (long long)p.B * p.strips;
     const long long rows = step ? p.B : p.items, gx = (rows + by - 1) / by;
     if (gx > 0x7fffffffLL || ny > 65535) return cudaErrorInvalidValue;
     const dim3 grid(static_cast<unsigned>(gx), ny), block(bx, by);
@@ -145,15 +174,19 @@ template <typename E, int VEC, int W> cudaError_t conv_run(ConvParams &p, bool s
         conv_kernel<E, VEC, W><<<grid, block, 0, stream>>>(p);
     return cudaGetLastError();
 }
-template <typename E, int VEC> cudaError_t conv_run_w(ConvParams &p, int W, bool step, cudaStream_t s) {
-    if (W == 2) return conv_run<E, VEC, 2>(p, step, s);
-    if (W == 3) return conv_run<E, VEC, 3>(p, step, s);
-    return conv_run<E, VEC, 4>(p, step, s);
+template <typename E, int VEC> cudaError_t conv_run_w(ConvParams &p, int W, bool step, int n_sm, cudaStream_t s) {
+    if (W == 2) return conv_run<E, VEC, 2>(p, step, n_sm, s);
+    if (W == 3) return conv_run<E, VEC, 3>(p, step, n_sm, s);
+    return conv_run<E, VEC, 4>(p, step, n_sm, s);
 }
-template <typename E> cudaError_t conv_run_e(ConvParams &p, int W, bool step, cudaStream_t s) {
-    constexpr int V = 16 / static_cast<int>(sizeof(E));
-    if (p.E % V == 0 && p.x_stride % V == 0) return conv_run_w<E, V>(p, W, step, s);
-    return conv_run_w<E, 1>(p, W, step, s);
+// Four channels a thread, two (16-bit elements) or one: what every row starts and ends on.  (Eight fp16 channels'
+// window, taps and loads do not fit the registers of 512 threads an SM.)
+template <typename E> cudaError_t conv_run_e(ConvParams &p, int W, bool step, int n_sm, cudaStream_t s) {
+    if (p.E % 4 == 0 && p.x_stride % 4 == 0) return conv_run_w<E, 4>(p, W, step, n_sm, s);
+    if constexpr (sizeof(E) == 2) {
+        if (p.E % 2 == 0 && p.x_stride % 2 == 0) return conv_run_w<E, 2>(p, W, step, n_sm, s);
+    }
+    return conv_run_w<E, 1>(p, W, step, n_sm, s);
 }
 
 }  // namespace
@@ -171,11 +204,12 @@ cudaError_t launch_conv(const ConvProblem &q, bool step, cudaStream_t stream) {
     p.B = q.B;
     p.E = q.E;
     p.silu = q.silu;
-    p.strips = (p.grid.T - 1) / kConvStrip + 1;
-    p.items = (long long)q.B * p.strips;
-    if (q.dtype == 0) return conv_run_e<float>(p, q.W, step, stream);
-    if (q.dtype == 1) return conv_run_e<__half>(p, q.W, step, stream);
-    return conv_run_e<__nv_bfloat16>(p, q.W, step, stream);
+    int n_sm = 0;
+    const cudaError_t e = sm_count(&n_sm);
+    if (e != cudaSuccess) return e;
+    if (q.dtype == 0) return conv_run_e<float>(p, q.W, step, n_sm, stream);
+    if (q.dtype == 1) return conv_run_e<__half>(p, q.W, step, n_sm, stream);
+    return conv_run_e<__nv_bfloat16>(p, q.W, step, n_sm, stream);
 }
 
 }  // namespace gtr

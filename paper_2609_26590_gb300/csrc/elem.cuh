@@ -35,12 +35,30 @@ template <> __device__ __forceinline__ uint32_t pack16<__nv_bfloat16>(float lo, 
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// VEC consecutive elements: 1, or the 16 bytes of an aligned vector.
+// VEC consecutive elements: 1, or an aligned vector of 4, 8 or 16 bytes.
 template <typename E, int VEC> struct Vec;
 template <typename E> struct Vec<E, 1> {
     using raw = E;
     static __device__ __forceinline__ void unpack(const raw &r, float (&f)[1]) { f[0] = to_f32(r); }
     static __device__ __forceinline__ raw pack(const float (&f)[1]) { return from_f32<E>(f[0]); }
+};
+template <typename E> struct Vec<E, 2> {  // 16-bit elements
+    using raw = uint32_t;
+    static __device__ __forceinline__ void unpack(const raw &r, float (&f)[2]) {
+        const float2 a = unpack16<E>(r);
+        f[0] = a.x, f[1] = a.y;
+    }
+    static __device__ __forceinline__ raw pack(const float (&f)[2]) { return pack16<E>(f[0], f[1]); }
+};
+template <typename E> struct Vec<E, 4> {  // 16-bit elements
+    using raw = uint2;
+    static __device__ __forceinline__ void unpack(const raw &r, float (&f)[4]) {
+        const float2 a = unpack16<E>(r.x), b = unpack16<E>(r.y);
+        f[0] = a.x, f[1] = a.y, f[2] = b.x, f[3] = b.y;
+    }
+    static __device__ __forceinline__ raw pack(const float (&f)[4]) {
+        return make_uint2(pack16<E>(f[0], f[1]), pack16<E>(f[2], f[3]));
+    }
 };
 template <> struct Vec<float, 4> {
     using raw = float4;
