@@ -25,6 +25,7 @@
 #include <cstring>
 
 #include "elem.cuh"
+#include "f32x2.cuh"
 #include "fastdiv.cuh"
 #include "gla_internal.h"
 #include "tc_ptx.cuh"
@@ -71,8 +72,19 @@ struct FfnBars {
     uint32_t tmem, abort;
 };
 
-// sigmoid by the hardware's 2^x and 1/x (a few 2^-22)
-__device__ __forceinline__ float sigmoid_hw(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+// The logistic function of a pair by the hardware's 2^x and 1/x (a few 2^-22).  Flushing their subnormal results
+// changes nothing: 1 + e is 1 there, and 1 / (1 + e) is below 2^-126.
+__device__ __forceinline__ f2 sigmoid2(f2 z) {
+    const float kNegLog2e = -1.4426950408889634f;
+    const float2 t = unpack2(mul2(z, pack2(kNegLog2e, kNegLog2e)));
+    float e0, e1, r0, r1;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(t.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(t.y));
+    const float2 d = unpack2(add2(pack2(e0, e1), pack2(1.f, 1.f)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(d.y));
+    return pack2(r0, r1);
+}
 
 template <int MODE, typename E>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_constant__ FfnParams p) {
@@ -223,32 +235,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
                     if (c == 1) {  // the accumulator is in registers
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive_cluster(acc_empty + 8 * buf);
+                        if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty + 8 * buf);
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {  // 16 bytes: eight columns
                         uint4 *at = reinterpret_cast<uint4 *>(box + lane * 128 + (((c * 4 + j) ^ (lane & 7)) << 4));
-                        float o0[8], o1[8];
-                        if constexpr (MODE == kFwd) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const float z = __uint_as_float(g[8 * j + i]);
-                                o0[i] = z * sigmoid_hw(z) * __uint_as_float(v[8 * j + i]);
-                            }
-                            *at = Vec<E, 8>::pack(o0);
-                        } else {
-                            float d[8];
-                            Vec<E, 8>::unpack(*at, d);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const float z = __uint_as_float(g[8 * j + i]), s = sigmoid_hw(z);
-                                const float ds = d[i] * s;
-                                o0[i] = ds * __uint_as_float(v[8 * j + i]) * fmaf(z, 1.f - s, 1.f);
-                                o1[i] = ds * z;
-                            }
-                            *at = Vec<E, 8>::pack(o0);
-                            *reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(at) + kBox) = Vec<E, 8>::pack(o1);
+                        uint32_t in[4], o0[4], o1[4];
+                        if constexpr (MODE == kAct) {
+                            const uint4 d = *at;
+                            in[0] = d.x, in[1] = d.y, in[2] = d.z, in[3] = d.w;
                         }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const f2 z = pack2(g[8 * j + 2 * i], g[8 * j + 2 * i + 1]);
+                            const f2 y = pack2(v[8 * j + 2 * i], v[8 * j + 2 * i + 1]), sg = sigmoid2(z);
+                            if constexpr (MODE == kFwd) {
+                                const float2 h = unpack2(mul2(mul2(z, sg), y));
+                                o0[i] = pack16<E>(h.x, h.y);
+                            } else {
+                                const float2 d = unpack16<E>(in[i]);
+                                const f2 one = pack2(1.f, 1.f), ds = mul2(pack2(d.x, d.y), sg);
+                                // dG = dH V s (1 + G (1 - s)), dV = dH s G
+                                const float2 dg = unpack2(mul2(mul2(ds, y), fma2(z, fma2(sg, pack2(-1.f, -1.f), one), one)));
+                                const float2 dv = unpack2(mul2(ds, z));
+                                o0[i] = pack16<E>(dg.x, dg.y);
+                                o1[i] = pack16<E>(dv.x, dv.y);
+                            }
+                        }
+                        *at = make_uint4(o0[0], o0[1], o0[2], o0[3]);
+                        if constexpr (MODE == kAct)
+                            *reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(at) + kBox) = make_uint4(o1[0], o1[1], o1[2], o1[3]);
                     }
                 }
                 fence_proxy_async_smem();
@@ -272,7 +288,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
                         if (c == 1 && b0 + 64 >= width) {
                             tc_fence_before();
                             __syncwarp();
-                            if (lane == 0) mbar_arrive_cluster(acc_empty + 8 * buf);
+                            if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty + 8 * buf);
                         }
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
