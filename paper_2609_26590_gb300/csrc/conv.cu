@@ -9,16 +9,20 @@
 // in registers; the scan order is in the walk's addresses.
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 #include "elem.cuh"
 #include "gla_internal.h"
 #include "scanpos.cuh"
+#include "tc_ptx.cuh"
 
 namespace gtr {
 namespace {
 
 constexpr int kConvThreads = 256;
 constexpr int kConvStrip = 32;  // most scan positions a thread walks
-constexpr int kConvBatch = 8;   // loads in flight
+constexpr int kConvBatch = 4;   // positions loaded at a time
+constexpr int kConvDepth = 4;   // batches in flight
 
 struct ConvParams {
     const void *x;
@@ -50,7 +54,7 @@ template <int VEC, int W> __device__ __forceinline__ void load_taps(const float 
 }
 
 template <typename E, int VEC, int W>
-__global__ void __launch_bounds__(kConvThreads, 2) conv_kernel(const __grid_constant__ ConvParams p) {
+__global__ void __launch_bounds__(kConvThreads, 3) conv_kernel(const __grid_constant__ ConvParams p) {
     using Raw = typename Vec<E, VEC>::raw;
     const long long item = (long long)blockIdx.x * blockDim.y + threadIdx.y;
     const int c = (blockIdx.y * blockDim.x + threadIdx.x) * VEC;
@@ -60,19 +64,45 @@ __global__ void __launch_bounds__(kConvThreads, 2) conv_kernel(const __grid_cons
     const E *x = static_cast<const E *>(p.x) + (long long)b * T * p.x_stride + c;
     const E *init = p.init ? static_cast<const E *>(p.init) + (long long)b * (W - 1) * p.E + c : nullptr;
     E *out = static_cast<E *>(p.out) + (long long)b * T * p.E + c;
+    // The positions ahead: copied to the thread's own slots of shared memory kConvDepth batches ahead (nothing but
+    // its own wait is between copy and use); single 16-bit elements, which cp.async does not copy, wait in
+    // registers, one batch ahead.
+    constexpr bool ASYNC = sizeof(Raw) >= 4;
+    extern __shared__ uint4 conv_smem[];
+    Raw *slots = reinterpret_cast<Raw *>(conv_smem) + threadIdx.y * blockDim.x + threadIdx.x;
+    const int stride = blockDim.x * blockDim.y;
     Raw in[kConvBatch];
     ScanPos ahead, pos;
     ahead.set(p.grid, s0);
     pos = ahead;
-    auto fetch = [&](int s) {
+    int fetched = s0, slot = 0;
+    auto fetch = [&] {
 #pragma unroll
         for (int k = 0; k < kConvBatch; ++k)
-            if (s + k < s1) {
-                in[k] = *reinterpret_cast<const Raw *>(x + (long long)ahead.t * p.x_stride);
+            if (fetched + k < s1) {
+                const E *src = x + (long long)ahead.t * p.x_stride;
+                if constexpr (!ASYNC)
+                    in[k] = *reinterpret_cast<const Raw *>(src);
+                else if constexpr (sizeof(Raw) == 16)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                                     ptx::smem_u32(slots + (slot * kConvBatch + k) * stride)),
+                                 "l"(src)
+                                 : "memory");
+                else
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(
+                                     ptx::smem_u32(slots + (slot * kConvBatch + k) * stride)),
+                                 "l"(src), "n"(sizeof(Raw))
+                                 : "memory");
                 ahead.next(p.grid);
             }
+        fetched += kConvBatch;
+        if constexpr (ASYNC) {
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            slot = slot + 1 == kConvDepth ? 0 : slot + 1;
+        }
     };
-    fetch(s0);
+#pragma unroll
+    for (int i = 0; i < (ASYNC ? kConvDepth : 1); ++i) fetch();
     float w[W][VEC], bias[VEC], win[W][VEC];  // win: inputs s - W + 1 .. s
     load_taps<VEC, W>(p.w + (long long)c * W, w);
 #pragma unroll
@@ -92,9 +122,15 @@ __global__ void __launch_bounds__(kConvThreads, 2) conv_kernel(const __grid_cons
     }
     for (int s = s0; s < s1; s += kConvBatch) {
         Raw now[kConvBatch];
+        if constexpr (ASYNC) asm volatile("cp.async.wait_group %0;" ::"n"(kConvDepth - 1) : "memory");
 #pragma unroll
-        for (int k = 0; k < kConvBatch; ++k) now[k] = in[k];
-        fetch(s + kConvBatch);
+        for (int k = 0; k < kConvBatch; ++k) {
+            if constexpr (ASYNC)
+                now[k] = slots[(slot * kConvBatch + k) * stride];  // (what no copy wrote is not used)
+            else
+                now[k] = in[k];
+        }
+        fetch();
 #pragma unroll
         for (int k = 0; k < kConvBatch; ++k) {
             if (s + k >= s1) break;
@@ -115,6 +151,7 @@ __global__ void __launch_bounds__(kConvThreads, 2) conv_kernel(const __grid_cons
             pos.next(p.grid);
         }
     }
+    if constexpr (ASYNC) asm volatile("cp.async.wait_all;" ::: "memory");
     if (p.state && s1 == T) {  // the window's last W - 1 inputs (exact: they are stored values)
         E *st = static_cast<E *>(p.state) + (long long)b * (W - 1) * p.E + c;
 #pragma unroll
@@ -156,6 +193,11 @@ __global__ void __launch_bounds__(kConvThreads) conv_step_kernel(const __grid_co
         *reinterpret_cast<typename Vec<E, VEC>::raw *>(st + (long long)j * p.E) = in[j + 1];
 }
 
+template <typename E, int VEC> size_t conv_smem_bytes(int threads) {  // at most 64 KB
+    const size_t raw = sizeof(typename Vec<E, VEC>::raw);
+    return raw >= 4 ? raw * kConvBatch * kConvDepth * threads : 0;
+}
+
 template <typename E, int VEC, int W> cudaError_t conv_run(ConvParams &p, bool step, int n_sm, cudaStream_t stream) {
     const int nv = (p.E + VEC - 1) / VEC;
     const int ny = (nv + kConvThreads - 1) / kConvThreads;
@@ -168,10 +210,23 @@ template <typename E, int VEC, int W> cudaError_t conv_run(ConvParams &p, bool s
     const long long rows = step ? p.B : p.items, gx = (rows + by - 1) / by;
     if (gx > 0x7fffffffLL || ny > 65535) return cudaErrorInvalidValue;
     const dim3 grid(static_cast<unsigned>(gx), ny), block(bx, by);
+    if (!step && conv_smem_bytes<E, VEC>(kConvThreads) > 48 * 1024) {
+        static std::atomic<unsigned long long> set_on_devices(0);
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        const unsigned long long bit = 1ull << (dev & 63);
+        if (!(set_on_devices.load(std::memory_order_relaxed) & bit)) {
+            e = cudaFuncSetAttribute(conv_kernel<E, VEC, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     static_cast<int>(conv_smem_bytes<E, VEC>(kConvThreads)));
+            if (e != cudaSuccess) return e;
+            set_on_devices.fetch_or(bit);
+        }
+    }
     if (step)
         conv_step_kernel<E, VEC, W><<<grid, block, 0, stream>>>(p);
     else
-        conv_kernel<E, VEC, W><<<grid, block, 0, stream>>>(p);
+        conv_kernel<E, VEC, W><<<grid, block, conv_smem_bytes<E, VEC>(bx * by), stream>>>(p);
     return cudaGetLastError();
 }
 template <typename E, int VEC> cudaError_t conv_run_w(ConvParams &p, int W, bool step, int n_sm, cudaStream_t s) {

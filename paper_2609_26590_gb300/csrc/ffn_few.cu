@@ -1,0 +1,158 @@
+// ffn_few.cu -- the gated feed-forward step for up to eight tokens (single tokens being served):
+//   out = SiLU(x Wg^T) * (x Wv^T)
+// on the CUDA cores.  With so few tokens the weights are all there is to move, 2 F D elements read once, and
+// a tensor-core tile of 128 rows would hold more padding than tokens.
+//
+// A CTA owns a contiguous range of channels and takes R of them at a time: its warps cut the 2 R weight
+// rows along D, 256 elements a warp in 16-byte loads, against their part of every token in registers (fp32
+// packed pairs); the next rows' loads are issued before the current sums are joined over the lanes (a halving
+// exchange).  The warps' sums of up to 64 / M channels meet in shared memory before one barrier, so that
+// between barriers every warp streams its weights alone; all sums are made in a fixed order.
+#include <cuda_runtime.h>
+
+#include "elem.cuh"
+#include "f32x2.cuh"
+#include "gla_internal.h"
+
+namespace gtr {
+namespace {
+
+struct FewParams {
+    const void *x, *wg, *wv;
+    void *out;
+    long long x_stride;
+    int M, D, F;
+};
+
+// Sum over the 32 lanes of N values each (N a power of two): lane l ends with the sum of value l / (32 / N).
+template <int N> __device__ __forceinline__ float lanes_sum(float (&v)[N]) {
+    const int lane = threadIdx.x & 31;
+    int n = N;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        if (n > 1) {
+            n /= 2;
+            const bool hi = lane & o;
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                if (i < n) {
+                    const float keep = hi ? v[i + n] : v[i], send = hi ? v[i] : v[i + n];
+                    v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+                }
+            }
+        } else {
+            v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+        }
+    }
+    return v[0];
+}
+
+template <typename E> __device__ __forceinline__ void widen8(const uint4 &r, f2 (&f)[4]) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 a = unpack16<E>(w[i]);
+        f[i] = pack2(a.x, a.y);
+    }
+}
+
+template <typename E, int M, int R>
+__global__ void __launch_bounds__(256, M <= 2 ? 2 : 1) ffn_few_kernel(const __grid_constant__ FewParams p) {
+    constexpr int N = 2 * R * M, PER = 32 / N;  // lanes that end with the same sum
+    constexpr int FB = 64 / M;                  // channels between barriers
+    static_assert(FB % R == 0 && 32 % N == 0, "whole groups");
+    __shared__ float part[8][2 * FB * M];
+    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int f_begin = static_cast<int>((long long)p.F * blockIdx.x / gridDim.x);
+    const int f_end = static_cast<int>((long long)p.F * (blockIdx.x + 1) / gridDim.x);
+    const int span = warps * 256, chunks = (p.D + span - 1) / span;  // elements of D the CTA takes at a time
+    const E *wg = static_cast<const E *>(p.wg), *wv = static_cast<const E *>(p.wv), *x = static_cast<const E *>(p.x);
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    f2 xs[M][4];
+    auto load_x = [&](int chunk) {
+        const int k = chunk * span + warp * 256 + lane * 8;
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+            widen8<E>(m < p.M && k < p.D ? *reinterpret_cast<const uint4 *>(x + m * p.x_stride + k) : zero, xs[m]);
+    };
+    uint4 next[2 * R];
+    auto load_w = [&](int f, int chunk) {
+        const int k = chunk * span + warp * 256 + lane * 8;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const bool in = f + r < f_end && k < p.D;
+            const long long at = (long long)(f + r) * p.D + k;
+            next[2 * r] = in ? *reinterpret_cast<const uint4 *>(wg + at) : zero;
+            next[2 * r + 1] = in ? *reinterpret_cast<const uint4 *>(wv + at) : zero;
+        }
+    };
+    load_w(f_begin, 0);
+    load_x(0);
+    for (int f0 = f_begin; f0 < f_end; f0 += FB) {
+        const int f1 = f_end - f0 < FB ? f_end : f0 + FB;
+        for (int f = f0; f < f1; f += R) {
+            f2 acc[N] = {};
+            for (int chunk = 0; chunk < chunks; ++chunk) {
+                uint4 now[2 * R];
+#pragma unroll
+                for (int i = 0; i < 2 * R; ++i) now[i] = next[i];
+                if (chunk + 1 < chunks)
+                    load_w(f, chunk + 1);
+                else if (f + R < f_end)
+                    load_w(f + R, 0);
+                if (chunks > 1) load_x(chunk);
+#pragma unroll
+                for (int i = 0; i < 2 * R; ++i) {
+                    f2 w[4];
+                    widen8<E>(now[i], w);
+#pragma unroll
+                    for (int m = 0; m < M; ++m)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[i * M + m] = fma2(w[j], xs[m][j], acc[i * M + m]);
+                }
+            }
+            float v[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float2 a = unpack2(acc[i]);
+                v[i] = a.x + a.y;
+            }
+            const float s = lanes_sum<N>(v);
+            if (lane % PER == 0) part[warp][(f - f0) * 2 * M + lane / PER] = s;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < (f1 - f0) * M; i += blockDim.x) {
+            const int r = i / M, m = i % M;
+            float g = 0.f, u = 0.f;
+            for (int w = 0; w < warps; ++w) g += part[w][2 * r * M + m], u += part[w][(2 * r + 1) * M + m];
+            if (m < p.M) static_cast<E *>(p.out)[(long long)m * p.F + f0 + r] = from_f32<E>(silu<E>(g) * u);
+        }
+        __syncthreads();
+    }
+}
+
+template <typename E, int M, int R> cudaError_t few_run(const FewParams &p, int n_sm, cudaStream_t stream) {
+    const int warps = p.D >= 2048 ? 8 : (p.D + 255) / 256;
+    const int per_sm = (M <= 2 ? 16 : 8) / warps, groups = (p.F + R - 1) / R;
+    const int grid = groups < n_sm * per_sm ? groups : n_sm * per_sm;
+    ffn_few_kernel<E, M, R><<<grid, 32 * warps, 0, stream>>>(p);
+    return cudaGetLastError();
+}
+template <typename E> cudaError_t few_run_m(const FewParams &p, int n_sm, cudaStream_t s) {
+    if (p.M == 1) return few_run<E, 1, 4>(p, n_sm, s);
+    if (p.M == 2) return few_run<E, 2, 4>(p, n_sm, s);
+    if (p.M <= 4) return few_run<E, 4, 4>(p, n_sm, s);
+    return few_run<E, 8, 2>(p, n_sm, s);
+}
+
+}  // namespace
+
+cudaError_t launch_ffn_few(const FfnProblem &q, void *out, cudaStream_t stream) {
+    int n_sm = 0;
+    const cudaError_t e = sm_count(&n_sm);
+    if (e != cudaSuccess) return e;
+    const FewParams p{q.x, q.w_gate, q.w_value, out, q.x_stride, static_cast<int>(q.M), q.D, q.F};
+    return q.dtype == 1 ? few_run_m<__half>(p, n_sm, stream) : few_run_m<__nv_bfloat16>(p, n_sm, stream);
+}
+
+}  // namespace gtr

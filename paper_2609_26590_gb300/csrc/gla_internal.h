@@ -174,6 +174,9 @@ struct FfnProblem {
     int dtype;                     // 1 f16, 2 bf16
 };
 bool ffn_supported(const FfnProblem &p);
+// Up to kFfnFewTokens tokens on the CUDA cores (ffn_few.cu), any number on the tensor cores (ffn.cu).
+constexpr int kFfnFewTokens = 8;
+cudaError_t launch_ffn_few(const FfnProblem &p, void *out, cudaStream_t stream);
 cudaError_t launch_ffn(const FfnProblem &p, void *out, cudaStream_t stream);
 // Scratch of the backward pass: dG and dV.
 size_t ffn_bwd_workspace(long long M, int F);

@@ -468,36 +468,62 @@ __global__ void __launch_bounds__(32 * kSsmMaxWarps, kSsmMinCtas) ssm_kernel(con
 }
 
 // One token of every sequence.  Memory-bound: the states are read and written once.  Four states a
-// thread in one 16-byte access, N / 4 neighbouring lanes a channel (N / 4 a power of two).
+// thread in one 16-byte access, N / 4 neighbouring lanes a channel (N / 4 a power of two), and the same
+// channels of kStepSeqs sequences, whose loads are issued together; A, D and the bias are read once for them.
+constexpr int kStepSeqs = 4;
 template <typename E, int LPC>
 __global__ void __launch_bounds__(256) ssm_step_kernel(const __grid_constant__ SsmParams p) {
     const int per = p.E * LPC;  // threads a sequence
     const int blocks = (per + 255) / 256;
-    const int b = blockIdx.x / blocks, i = (blockIdx.x - b * blocks) * 256 + threadIdx.x;
+    const int group = blockIdx.x / blocks, i = (blockIdx.x - group * blocks) * 256 + threadIdx.x;
     const bool live = i < per;
-    const int c = live ? i / LPC : 0, q = i % LPC;
-    const float u = to_f32(static_cast<const E *>(p.x)[(long long)b * p.x_stride + c]);
-    float dt = to_f32(static_cast<const E *>(p.delta)[(long long)b * p.delta_stride + c]) + (p.bias ? p.bias[c] : 0.f);
-    if (p.softplus) dt = softplus(dt);
-    const long long at = ((long long)b * p.E + c) * (4 * LPC) + 4 * q;
-    const float4 a = *reinterpret_cast<const float4 *>(p.A + (long long)c * (4 * LPC) + 4 * q);
-    const float4 h = *reinterpret_cast<const float4 *>(p.init + at);
-    const E *Bm = static_cast<const E *>(p.Bm) + (long long)b * p.b_stride + 4 * q;
-    const E *C = static_cast<const E *>(p.C) + (long long)b * p.c_stride + 4 * q;
-    const float du = dt * u, av[4] = {a.x, a.y, a.z, a.w}, hv[4] = {h.x, h.y, h.z, h.w};
-    float n[4], y = 0.f;
+    const int c = live ? i / LPC : 0, q = i % LPC, b0 = group * kStepSeqs;
+    float4 h[kStepSeqs];
+    float u[kStepSeqs], v[kStepSeqs], zv[kStepSeqs], bv[kStepSeqs][4], cv[kStepSeqs][4];
+    const bool quads = (reinterpret_cast<uintptr_t>(p.Bm) | reinterpret_cast<uintptr_t>(p.C)) % (4 * sizeof(E)) == 0 &&
+                       p.b_stride % 4 == 0 && p.c_stride % 4 == 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        n[k] = fmaf(exp2_hw(dt * (av[k] * kLog2e)), hv[k], du * to_f32(Bm[k]));
-        y = fmaf(to_f32(C[k]), n[k], y);
+    for (int k = 0; k < kStepSeqs; ++k) {
+        const int b = b0 + k < p.B ? b0 + k : p.B - 1;  // (the last sequence again: not stored)
+        h[k] = *reinterpret_cast<const float4 *>(p.init + ((long long)b * p.E + c) * (4 * LPC) + 4 * q);
+        u[k] = to_f32(static_cast<const E *>(p.x)[(long long)b * p.x_stride + c]);
+        v[k] = to_f32(static_cast<const E *>(p.delta)[(long long)b * p.delta_stride + c]);
+        zv[k] = p.z ? to_f32(static_cast<const E *>(p.z)[(long long)b * p.z_stride + c]) : 0.f;
+        const E *Bm = static_cast<const E *>(p.Bm) + (long long)b * p.b_stride + 4 * q;
+        const E *C = static_cast<const E *>(p.C) + (long long)b * p.c_stride + 4 * q;
+        if (quads) {
+            const float4 f = ld_quad<E>(Bm), g = ld_quad<E>(C);
+            bv[k][0] = f.x, bv[k][1] = f.y, bv[k][2] = f.z, bv[k][3] = f.w;
+            cv[k][0] = g.x, cv[k][1] = g.y, cv[k][2] = g.z, cv[k][3] = g.w;
+        } else {
+#pragma unroll
+            for (int n = 0; n < 4; ++n) bv[k][n] = to_f32(Bm[n]), cv[k][n] = to_f32(C[n]);
+        }
     }
-    if (live) *reinterpret_cast<float4 *>(p.state + at) = make_float4(n[0], n[1], n[2], n[3]);
+    const float4 a = *reinterpret_cast<const float4 *>(p.A + (long long)c * (4 * LPC) + 4 * q);
+    const float av[4] = {a.x * kLog2e, a.y * kLog2e, a.z * kLog2e, a.w * kLog2e};
+    const float bias = p.bias ? p.bias[c] : 0.f, skip = p.D ? p.D[c] : 0.f;
 #pragma unroll
-    for (int o = LPC / 2; o > 0; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
-    if (live && q == 0) {
-        if (p.D) y = fmaf(p.D[c], u, y);
-        if (p.z) y *= silu<E>(to_f32(static_cast<const E *>(p.z)[(long long)b * p.z_stride + c]));
-        static_cast<E *>(p.out)[(long long)b * p.E + c] = from_f32<E>(y);
+    for (int k = 0; k < kStepSeqs; ++k) {
+        const int b = b0 + k;
+        float dt = v[k] + bias;
+        if (p.softplus) dt = softplus(dt);
+        const float du = dt * u[k], hv[4] = {h[k].x, h[k].y, h[k].z, h[k].w};
+        float n[4], y = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            n[j] = fmaf(exp2_hw(dt * av[j]), hv[j], du * bv[k][j]);
+            y = fmaf(cv[k][j], n[j], y);
+        }
+        if (live && b < p.B)
+            *reinterpret_cast<float4 *>(p.state + ((long long)b * p.E + c) * (4 * LPC) + 4 * q) = make_float4(n[0], n[1], n[2], n[3]);
+#pragma unroll
+        for (int o = LPC / 2; o > 0; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
+        if (live && b < p.B && q == 0) {
+            y = fmaf(skip, u[k], y);
+            if (p.z) y *= silu<E>(zv[k]);
+            static_cast<E *>(p.out)[(long long)b * p.E + c] = from_f32<E>(y);
+        }
     }
 }
 
@@ -662,9 +688,11 @@ template <typename E> cudaError_t ssm_run(SsmParams &p, cudaStream_t s) {
 
 template <typename E> cudaError_t ssm_step_e(SsmParams &p, cudaStream_t s) {
     const int lpc = p.N % 4 == 0 ? p.N / 4 : 0;
-    const long long per = lpc && !(lpc & (lpc - 1)) ? ((long long)p.E * lpc + 255) / 256 : ((long long)p.E + 127) / 128;
-    if (per * p.B > 0x7fffffffLL) return cudaErrorInvalidValue;
-    const unsigned ctas = static_cast<unsigned>(per * p.B);
+    const bool quads = lpc && !(lpc & (lpc - 1));
+    const long long per = quads ? ((long long)p.E * lpc + 255) / 256 : ((long long)p.E + 127) / 128;
+    const long long rows = quads ? (p.B + kStepSeqs - 1) / kStepSeqs : p.B;
+    if (per * rows > 0x7fffffffLL) return cudaErrorInvalidValue;
+    const unsigned ctas = static_cast<unsigned>(per * rows);
     switch (lpc) {
     case 1: ssm_step_kernel<E, 1><<<ctas, 256, 0, s>>>(p); break;
     case 2: ssm_step_kernel<E, 2><<<ctas, 256, 0, s>>>(p); break;

@@ -435,7 +435,10 @@ def forward_lowrank_gate(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, a_lo
 # ------------------------------------------------------------------ the operators around the mixer
 #
 # Outputs and workspaces that a call allocates belong to the stream it runs on (``stream``, else the
-# current one), so the caching allocator hands their memory on only behind that stream's work.
+# current one), so the caching allocator hands their memory on only behind that stream's work.  The checks
+# are written for the case that passes: a small call's kernel takes 2 us, and every query of a tensor 0.1 to 0.3.
+
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _code(t: torch.Tensor) -> int:
@@ -445,41 +448,54 @@ def _code(t: torch.Tensor) -> int:
     return code
 
 
-def _on_device(first: torch.Tensor, **tensors) -> None:
-    """Every tensor lies on the current CUDA device (kernels and allocations go there)."""
-    for name, t in tensors.items():
-        if t is not None and (not t.is_cuda or t.device != first.device):
-            raise ValueError(f"{name} must be a CUDA tensor on the other inputs' device")
-    if first.device.index != torch._C._cuda_getDevice():
-        raise ValueError(f"the tensors are on {first.device}, which is not the current device")
+def _on_device(*tensors) -> None:
+    """Every tensor (None: left out) lies on the current CUDA device, where kernels and allocations go."""
+    first = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and (t.get_device() != first or first < 0):
+            raise ValueError("every tensor must be a CUDA tensor, all of them on one device")
+    if first != _current_device():
+        raise ValueError(f"the tensors are on cuda:{first}, which is not the current device")
 
 
 def _like(t: torch.Tensor, dtype: torch.dtype, shape, name: str) -> None:
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {list(shape)} {str(dtype).split('.')[1]} tensor")
 
 
-def _new(given: Optional[torch.Tensor], shape, dtype: torch.dtype, device, stream, name: str) -> torch.Tensor:
+def _vector(t: Optional[torch.Tensor], n: int, name: str):
+    """Address of a [n] float32 tensor, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{n}] float32 tensor")
+    return t.data_ptr()
+
+
+def _new(given: Optional[torch.Tensor], shape, dtype: torch.dtype, like: torch.Tensor, stream, name: str) -> torch.Tensor:
     """The caller's tensor, checked, or a new one whose memory belongs to the call's stream."""
     if given is not None:
         _like(given, dtype, shape, name)
-        if given.device != device:
+        if given.get_device() != like.get_device():
             raise ValueError(f"{name} must be on the inputs' device")
         return given
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _row_stride(t: torch.Tensor, name: str) -> int:
     """Elements from one row (all leading dimensions flattened) to the next; the last dimension is
     contiguous and the leading ones collapse into one."""
-    width, n = t.shape[-1], t.numel() // max(t.shape[-1], 1)
+    shape = t.shape
+    width = shape[-1]
+    if t.is_contiguous():
+        return width
     if width != 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
     stride = span = None
-    for size, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+    for size, st in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
         if size == 1:
             continue
         if stride is None:
@@ -487,7 +503,7 @@ def _row_stride(t: torch.Tensor, name: str) -> int:
         elif st != span:
             raise ValueError(f"{name}'s leading dimensions must collapse into one token stride")
         span = st * size
-    if stride is None or n <= 1:
+    if stride is None:
         return width
     if stride < width:
         raise ValueError(f"{name}'s tokens overlap")
@@ -498,26 +514,28 @@ def _ptr(t: Optional[torch.Tensor]):
     return t.data_ptr() if t is not None else None
 
 
+def _nbytes(t: Optional[torch.Tensor]) -> int:
+    return t.numel() * t.element_size() if t is not None else 0
+
+
 def layernorm(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], eps: float,
               stats: bool = False, out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Layer norm over the last dimension through ``gtr_layernorm_fwd``.  x: [..., D] (contiguous last
     dimension, one token stride); weight, bias: [D] float32 or None.  Returns out like x (contiguous), with
     ``stats`` (out, mean, rstd): float32 of x's leading shape, what :func:`layernorm_backward` reads."""
-    lib, code = load(), _code(x)
-    D, dev = x.shape[-1], x.device
-    _on_device(x, x=x, weight=weight, bias=bias)
-    for name, t in (("weight", weight), ("bias", bias)):
-        if t is not None:
-            _like(t, torch.float32, (D,), name)
-    xs = _row_stride(x, "x")
-    out = _new(out, x.shape, x.dtype, dev, stream, "out")
+    lib, code, shape = load(), _code(x), x.shape
+    D = shape[-1]
+    _on_device(x, weight, bias)
+    out = _new(out, shape, x.dtype, x, stream, "out")
     mean = rstd = None
     if stats:
-        mean = _new(None, x.shape[:-1], torch.float32, dev, stream, "mean")
-        rstd = _new(None, x.shape[:-1], torch.float32, dev, stream, "rstd")
-    status = lib.gtr_layernorm_fwd(x.data_ptr(), xs, _ptr(weight), _ptr(bias), float(eps), x.numel() // max(D, 1), D, code,
-                                   out.data_ptr(), _ptr(mean), _ptr(rstd), _stream_ptr(stream))
-    _check(status, "gtr_layernorm_fwd", lib)
+        mean = _new(None, shape[:-1], torch.float32, x, stream, "mean")
+        rstd = _new(None, shape[:-1], torch.float32, x, stream, "rstd")
+    status = lib.gtr_layernorm_fwd(x.data_ptr(), _row_stride(x, "x"), _vector(weight, D, "weight"), _vector(bias, D, "bias"),
+                                   float(eps), x.numel() // D if D else 0, D, code, out.data_ptr(), _ptr(mean), _ptr(rstd),
+                                   _stream_ptr(stream))
+    if status:
+        _check(status, "gtr_layernorm_fwd", lib)
     return (out, mean, rstd) if stats else out
 
 
@@ -527,32 +545,27 @@ def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch
     """Backward pass of :func:`layernorm` through ``gtr_layernorm_bwd``: (dx, dweight, dbias) for the gradient
     dy of its output; dweight and dbias ([D] float32) are None when weight is None.  ``workspace``: a CUDA uint8
     tensor of at least ``layernorm_backward_workspace_bytes()`` that no overlapping call shares."""
-    lib, code = load(), _code(x)
-    D, dev = x.shape[-1], x.device
-    _on_device(x, x=x, dy=dy, weight=weight, mean=mean, rstd=rstd, workspace=workspace)
-    if dy.shape != x.shape or dy.dtype != x.dtype:
+    lib, code, shape = load(), _code(x), x.shape
+    D = shape[-1]
+    _on_device(x, dy, weight, mean, rstd, workspace)
+    if dy.shape != shape or dy.dtype != x.dtype:
         raise ValueError("dy must have x's shape and dtype")
-    if weight is not None:
-        _like(weight, torch.float32, (D,), "weight")
-    _like(mean, torch.float32, x.shape[:-1], "mean")
-    _like(rstd, torch.float32, x.shape[:-1], "rstd")
-    xs, ds, n = _row_stride(x, "x"), _row_stride(dy, "dy"), x.numel() // max(D, 1)
-    dx = _new(None, x.shape, x.dtype, dev, stream, "dx")
+    _like(mean, torch.float32, shape[:-1], "mean")
+    _like(rstd, torch.float32, shape[:-1], "rstd")
+    n = x.numel() // D if D else 0
+    dx = _new(None, shape, x.dtype, x, stream, "dx")
     dw = db = None
     if weight is not None:
-        dw = _new(None, (D,), torch.float32, dev, stream, "dweight")
-        db = _new(None, (D,), torch.float32, dev, stream, "dbias")
+        dw = _new(None, (D,), torch.float32, x, stream, "dweight")
+        db = _new(None, (D,), torch.float32, x, stream, "dbias")
         if workspace is None:
-            workspace = _new(None, (layernorm_backward_workspace_bytes(n, D),), torch.uint8, dev, stream, "workspace")
-    status = lib.gtr_layernorm_bwd(dy.data_ptr(), ds, x.data_ptr(), xs, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), n, D,
-                                   code, dx.data_ptr(), _ptr(dw), _ptr(db), _ptr(workspace), _nbytes(workspace),
-                                   _stream_ptr(stream))
-    _check(status, "gtr_layernorm_bwd", lib)
+            workspace = _new(None, (lib.gtr_layernorm_bwd_workspace_bytes(n, D),), torch.uint8, x, stream, "workspace")
+    status = lib.gtr_layernorm_bwd(dy.data_ptr(), _row_stride(dy, "dy"), x.data_ptr(), _row_stride(x, "x"),
+                                   _vector(weight, D, "weight"), mean.data_ptr(), rstd.data_ptr(), n, D, code, dx.data_ptr(),
+                                   _ptr(dw), _ptr(db), _ptr(workspace), _nbytes(workspace), _stream_ptr(stream))
+    if status:
+        _check(status, "gtr_layernorm_bwd", lib)
     return dx, dw, db
-
-
-def _nbytes(t: Optional[torch.Tensor]) -> int:
-    return t.numel() * t.element_size() if t is not None else 0
 
 
 def layernorm_backward_workspace_bytes(n: int, D: int) -> int:
@@ -577,20 +590,19 @@ def causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tens
     lib, code = load(), _code(x)
     B, T, E = _sequence(x, grid_h, grid_w)
     W = weight.shape[-1]
-    _on_device(x, x=x, weight=weight, bias=bias, initial_state=initial_state)
+    _on_device(x, weight, bias, initial_state)
     _like(weight, torch.float32, (E, W), "weight")
-    if bias is not None:
-        _like(bias, torch.float32, (E,), "bias")
     if initial_state is not None:
         _like(initial_state, x.dtype, (B, W - 1, E), "initial_state")
-    xs = _row_stride(x, "x")
-    out = _new(out, (B, T, E), x.dtype, x.device, stream, "out")
+    out = _new(out, (B, T, E), x.dtype, x, stream, "out")
     fs = None
     if final_state is not None and final_state is not False:
-        fs = _new(None if final_state is True else final_state, (B, W - 1, E), x.dtype, x.device, stream, "final_state")
-    status = lib.gtr_causal_conv_fwd(x.data_ptr(), xs, weight.data_ptr(), _ptr(bias), int(bool(silu)), _ptr(initial_state),
-                                     B, grid_h, grid_w, E, W, order, code, out.data_ptr(), _ptr(fs), _stream_ptr(stream))
-    _check(status, "gtr_causal_conv_fwd", lib)
+        fs = _new(None if final_state is True else final_state, (B, W - 1, E), x.dtype, x, stream, "final_state")
+    status = lib.gtr_causal_conv_fwd(x.data_ptr(), _row_stride(x, "x"), weight.data_ptr(), _vector(bias, E, "bias"),
+                                     1 if silu else 0, _ptr(initial_state), B, grid_h, grid_w, E, W, order, code,
+                                     out.data_ptr(), _ptr(fs), _stream_ptr(stream))
+    if status:
+        _check(status, "gtr_causal_conv_fwd", lib)
     return out, fs
 
 
@@ -604,35 +616,35 @@ def causal_conv_step(x: torch.Tensor, state: torch.Tensor, weight: torch.Tensor,
         raise ValueError("x must be [B, E]")
     B, E = x.shape
     W = weight.shape[-1]
-    _on_device(x, x=x, state=state, weight=weight, bias=bias)
+    _on_device(x, state, weight, bias)
     _like(weight, torch.float32, (E, W), "weight")
-    if bias is not None:
-        _like(bias, torch.float32, (E,), "bias")
     _like(state, x.dtype, (B, W - 1, E), "state")
-    new = _new(state if state_out is None else state_out, state.shape, x.dtype, x.device, stream, "state_out")
-    out = _new(out, (B, E), x.dtype, x.device, stream, "out")
-    status = lib.gtr_causal_conv_step(x.data_ptr(), _row_stride(x, "x"), state.data_ptr(), weight.data_ptr(), _ptr(bias),
-                                      int(bool(silu)), B, E, W, code, out.data_ptr(), new.data_ptr(), _stream_ptr(stream))
-    _check(status, "gtr_causal_conv_step", lib)
+    new = state if state_out is None else _new(state_out, (B, W - 1, E), x.dtype, x, stream, "state_out")
+    out = _new(out, (B, E), x.dtype, x, stream, "out")
+    status = lib.gtr_causal_conv_step(x.data_ptr(), _row_stride(x, "x"), state.data_ptr(), weight.data_ptr(),
+                                      _vector(bias, E, "bias"), 1 if silu else 0, B, E, W, code, out.data_ptr(),
+                                      new.data_ptr(), _stream_ptr(stream))
+    if status:
+        _check(status, "gtr_causal_conv_step", lib)
     return out, new
 
 
-def _ssm_args(lead, x, delta, A, Bm, C, D, z, delta_bias):
-    E, N = x.shape[-1], A.shape[-1]
-    _on_device(x, x=x, delta=delta, A=A, Bm=Bm, C=C, D=D, z=z, delta_bias=delta_bias)
+def _ssm_row(t, shape, dtype, name: str):
+    """(address, token stride) of one of the scan's per-token inputs."""
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be {list(shape)} of x's dtype")
+    return t.data_ptr(), _row_stride(t, name)
+
+
+def _ssm_args(x, delta, A, Bm, C, D, z, delta_bias):
+    """The arguments that the scan and its single step share, in the library's order."""
+    shape, dtype = x.shape, x.dtype
+    E, N = shape[-1], A.shape[-1]
     _like(A, torch.float32, (E, N), "A")
-    for name, t in (("D", D), ("delta_bias", delta_bias)):
-        if t is not None:
-            _like(t, torch.float32, (E,), name)
-    strides = []
-    for name, t, width in (("x", x, E), ("delta", delta, E), ("z", z, E), ("Bm", Bm, N), ("C", C, N)):
-        if t is None:
-            strides.append(0)
-            continue
-        if tuple(t.shape) != (*lead, width) or t.dtype != x.dtype:
-            raise ValueError(f"{name} must be {[*lead, width]} of x's dtype")
-        strides.append(_row_stride(t, name))
-    return E, N, strides
+    bc = shape[:-1] + (N,)
+    return (N, (x.data_ptr(), _row_stride(x, "x"), *_ssm_row(delta, shape, dtype, "delta"), A.data_ptr(),
+                *_ssm_row(Bm, bc, dtype, "Bm"), *_ssm_row(C, bc, dtype, "C"), _vector(D, E, "D"),
+                *(_ssm_row(z, shape, dtype, "z") if z is not None else (None, 0)), _vector(delta_bias, E, "delta_bias")))
 
 
 def ssm_scan(x: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, Bm: torch.Tensor, C: torch.Tensor, grid_h: int,
@@ -646,18 +658,18 @@ def ssm_scan(x: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, Bm: torch.Te
     (out [B, T, E], final_state)."""
     lib, code = load(), _code(x)
     B, T, E = _sequence(x, grid_h, grid_w)
-    E, N, (xs, ds, zs, bs, cs) = _ssm_args((B, T), x, delta, A, Bm, C, D, z, delta_bias)
+    _on_device(x, delta, A, Bm, C, D, z, delta_bias, initial_state)
+    N, args = _ssm_args(x, delta, A, Bm, C, D, z, delta_bias)
     if initial_state is not None:
-        _on_device(x, initial_state=initial_state)
         _like(initial_state, torch.float32, (B, E, N), "initial_state")
-    out = _new(out, (B, T, E), x.dtype, x.device, stream, "out")
+    out = _new(out, (B, T, E), x.dtype, x, stream, "out")
     fs = None
     if final_state is not None and final_state is not False:
-        fs = _new(None if final_state is True else final_state, (B, E, N), torch.float32, x.device, stream, "final_state")
-    status = lib.gtr_ssm_scan_fwd(x.data_ptr(), xs, delta.data_ptr(), ds, A.data_ptr(), Bm.data_ptr(), bs, C.data_ptr(), cs,
-                                  _ptr(D), _ptr(z), zs, _ptr(delta_bias), int(bool(softplus)), _ptr(initial_state), B,
-                                  grid_h, grid_w, E, N, order, code, out.data_ptr(), _ptr(fs), _stream_ptr(stream))
-    _check(status, "gtr_ssm_scan_fwd", lib)
+        fs = _new(None if final_state is True else final_state, (B, E, N), torch.float32, x, stream, "final_state")
+    status = lib.gtr_ssm_scan_fwd(*args, 1 if softplus else 0, _ptr(initial_state), B, grid_h, grid_w, E, N, order, code,
+                                  out.data_ptr(), _ptr(fs), _stream_ptr(stream))
+    if status:
+        _check(status, "gtr_ssm_scan_fwd", lib)
     return out, fs
 
 
@@ -671,28 +683,27 @@ def ssm_step(x: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, Bm: torch.Te
     lib, code = load(), _code(x)
     if x.dim() != 2:
         raise ValueError("x must be [B, E]")
-    B = x.shape[0]
-    E, N, (xs, ds, zs, bs, cs) = _ssm_args((B,), x, delta, A, Bm, C, D, z, delta_bias)
-    _on_device(x, state=state)
+    B, E = x.shape
+    _on_device(x, delta, A, Bm, C, D, z, delta_bias, state)
+    N, args = _ssm_args(x, delta, A, Bm, C, D, z, delta_bias)
     _like(state, torch.float32, (B, E, N), "state")
-    new = _new(state if state_out is None else state_out, state.shape, torch.float32, x.device, stream, "state_out")
-    out = _new(out, (B, E), x.dtype, x.device, stream, "out")
-    status = lib.gtr_ssm_step(x.data_ptr(), xs, delta.data_ptr(), ds, A.data_ptr(), Bm.data_ptr(), bs, C.data_ptr(), cs,
-                              _ptr(D), _ptr(z), zs, _ptr(delta_bias), int(bool(softplus)), state.data_ptr(), B, E, N, code,
-                              out.data_ptr(), new.data_ptr(), _stream_ptr(stream))
-    _check(status, "gtr_ssm_step", lib)
+    new = state if state_out is None else _new(state_out, (B, E, N), torch.float32, x, stream, "state_out")
+    out = _new(out, (B, E), x.dtype, x, stream, "out")
+    status = lib.gtr_ssm_step(*args, 1 if softplus else 0, state.data_ptr(), B, E, N, code, out.data_ptr(), new.data_ptr(),
+                              _stream_ptr(stream))
+    if status:
+        _check(status, "gtr_ssm_step", lib)
     return out, new
 
 
 def _ffn_args(x, w_gate, w_value):
     code = _code(x)
-    if x.dtype == torch.float32:
+    if code == 0:
         raise GLAError(2, "gtr_swiglu_ffn: float16 or bfloat16 only")
     D, F = x.shape[-1], w_gate.shape[0]
-    _on_device(x, x=x, w_gate=w_gate, w_value=w_value)
     _like(w_gate, x.dtype, (F, D), "w_gate")
     _like(w_value, x.dtype, (F, D), "w_value")
-    return code, x.numel() // max(D, 1), D, F, _row_stride(x, "x")
+    return code, x.numel() // D if D else 0, D, F
 
 
 def swiglu_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_value: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -700,11 +711,13 @@ def swiglu_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_value: torch.Tensor, out
     """Gated feed-forward step through ``gtr_swiglu_ffn_fwd``: SiLU(x w_gate^T) * (x w_value^T).  x: [..., D];
     w_gate, w_value: [F, D]; one dtype, float16 or bfloat16; D and F multiples of 8.  Returns [..., F]."""
     lib = load()
-    code, M, D, F, xs = _ffn_args(x, w_gate, w_value)
-    out = _new(out, (*x.shape[:-1], F), x.dtype, x.device, stream, "out")
-    status = lib.gtr_swiglu_ffn_fwd(x.data_ptr(), xs, w_gate.data_ptr(), w_value.data_ptr(), M, D, F, code, out.data_ptr(),
-                                    _stream_ptr(stream))
-    _check(status, "gtr_swiglu_ffn_fwd", lib)
+    code, M, D, F = _ffn_args(x, w_gate, w_value)
+    _on_device(x, w_gate, w_value)
+    out = _new(out, x.shape[:-1] + (F,), x.dtype, x, stream, "out")
+    status = lib.gtr_swiglu_ffn_fwd(x.data_ptr(), _row_stride(x, "x"), w_gate.data_ptr(), w_value.data_ptr(), M, D, F, code,
+                                    out.data_ptr(), _stream_ptr(stream))
+    if status:
+        _check(status, "gtr_swiglu_ffn_fwd", lib)
     return out
 
 
@@ -720,19 +733,20 @@ def swiglu_ffn_backward(dout: torch.Tensor, x: torch.Tensor, w_gate: torch.Tenso
     dout of its output, in the inputs' dtype.  ``workspace``: a CUDA uint8 tensor of at least
     ``swiglu_ffn_backward_workspace_bytes()`` that no overlapping call shares."""
     lib = load()
-    code, M, D, F, xs = _ffn_args(x, w_gate, w_value)
-    _on_device(x, dout=dout, workspace=workspace)
-    if tuple(dout.shape) != (*x.shape[:-1], F) or dout.dtype != x.dtype:
+    code, M, D, F = _ffn_args(x, w_gate, w_value)
+    _on_device(x, dout, w_gate, w_value, workspace)
+    if dout.shape != x.shape[:-1] + (F,) or dout.dtype != x.dtype:
         raise ValueError("dout must be [..., F] of x's leading shape and dtype")
-    dx = _new(None, x.shape, x.dtype, x.device, stream, "dx")
-    dwg = _new(None, (F, D), x.dtype, x.device, stream, "dw_gate")
-    dwv = _new(None, (F, D), x.dtype, x.device, stream, "dw_value")
+    dx = _new(None, x.shape, x.dtype, x, stream, "dx")
+    dwg = _new(None, (F, D), x.dtype, x, stream, "dw_gate")
+    dwv = _new(None, (F, D), x.dtype, x, stream, "dw_value")
     if workspace is None:
-        workspace = _new(None, (swiglu_ffn_backward_workspace_bytes(M, D, F),), torch.uint8, x.device, stream, "workspace")
-    status = lib.gtr_swiglu_ffn_bwd(dout.data_ptr(), _row_stride(dout, "dout"), x.data_ptr(), xs, w_gate.data_ptr(),
-                                    w_value.data_ptr(), M, D, F, code, dx.data_ptr(), dwg.data_ptr(), dwv.data_ptr(),
-                                    workspace.data_ptr(), _nbytes(workspace), _stream_ptr(stream))
-    _check(status, "gtr_swiglu_ffn_bwd", lib)
+        workspace = _new(None, (lib.gtr_swiglu_ffn_bwd_workspace_bytes(M, D, F),), torch.uint8, x, stream, "workspace")
+    status = lib.gtr_swiglu_ffn_bwd(dout.data_ptr(), _row_stride(dout, "dout"), x.data_ptr(), _row_stride(x, "x"),
+                                    w_gate.data_ptr(), w_value.data_ptr(), M, D, F, code, dx.data_ptr(), dwg.data_ptr(),
+                                    dwv.data_ptr(), workspace.data_ptr(), _nbytes(workspace), _stream_ptr(stream))
+    if status:
+        _check(status, "gtr_swiglu_ffn_bwd", lib)
     return dx, dwg, dwv
 
 
