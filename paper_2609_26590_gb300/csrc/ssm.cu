@@ -471,33 +471,34 @@ __global__ void __launch_bounds__(32 * kSsmMaxWarps, kSsmMinCtas) ssm_kernel(con
 // thread in one 16-byte access, N / 4 neighbouring lanes a channel (N / 4 a power of two), and the same
 // channels of kStepSeqs sequences, whose loads are issued together; A, D and the bias are read once for them.
 constexpr int kStepSeqs = 4;
-template <typename E, int LPC>
-__global__ void __launch_bounds__(256) ssm_step_kernel(const __grid_constant__ SsmParams p) {
+template <typename E, int LPC, bool QUADS>  // QUADS: B and C start on four elements
+__global__ void __launch_bounds__(256, 4) ssm_step_kernel(const __grid_constant__ SsmParams p) {
+    using Four = typename Vec<E, 4>::raw;
     const int per = p.E * LPC;  // threads a sequence
     const int blocks = (per + 255) / 256;
     const int group = blockIdx.x / blocks, i = (blockIdx.x - group * blocks) * 256 + threadIdx.x;
     const bool live = i < per;
     const int c = live ? i / LPC : 0, q = i % LPC, b0 = group * kStepSeqs;
     float4 h[kStepSeqs];
-    float u[kStepSeqs], v[kStepSeqs], zv[kStepSeqs], bv[kStepSeqs][4], cv[kStepSeqs][4];
-    const bool quads = (reinterpret_cast<uintptr_t>(p.Bm) | reinterpret_cast<uintptr_t>(p.C)) % (4 * sizeof(E)) == 0 &&
-                       p.b_stride % 4 == 0 && p.c_stride % 4 == 0;
+    E u[kStepSeqs], v[kStepSeqs], zv[kStepSeqs];
+    Four bq[kStepSeqs], cq[kStepSeqs];
 #pragma unroll
     for (int k = 0; k < kStepSeqs; ++k) {
         const int b = b0 + k < p.B ? b0 + k : p.B - 1;  // (the last sequence again: not stored)
         h[k] = *reinterpret_cast<const float4 *>(p.init + ((long long)b * p.E + c) * (4 * LPC) + 4 * q);
-        u[k] = to_f32(static_cast<const E *>(p.x)[(long long)b * p.x_stride + c]);
-        v[k] = to_f32(static_cast<const E *>(p.delta)[(long long)b * p.delta_stride + c]);
-        zv[k] = p.z ? to_f32(static_cast<const E *>(p.z)[(long long)b * p.z_stride + c]) : 0.f;
+        u[k] = static_cast<const E *>(p.x)[(long long)b * p.x_stride + c];
+        v[k] = static_cast<const E *>(p.delta)[(long long)b * p.delta_stride + c];
+        if (p.z) zv[k] = static_cast<const E *>(p.z)[(long long)b * p.z_stride + c];
         const E *Bm = static_cast<const E *>(p.Bm) + (long long)b * p.b_stride + 4 * q;
         const E *C = static_cast<const E *>(p.C) + (long long)b * p.c_stride + 4 * q;
-        if (quads) {
-            const float4 f = ld_quad<E>(Bm), g = ld_quad<E>(C);
-            bv[k][0] = f.x, bv[k][1] = f.y, bv[k][2] = f.z, bv[k][3] = f.w;
-            cv[k][0] = g.x, cv[k][1] = g.y, cv[k][2] = g.z, cv[k][3] = g.w;
+        if constexpr (QUADS) {
+            bq[k] = *reinterpret_cast<const Four *>(Bm);
+            cq[k] = *reinterpret_cast<const Four *>(C);
         } else {
-#pragma unroll
-            for (int n = 0; n < 4; ++n) bv[k][n] = to_f32(Bm[n]), cv[k][n] = to_f32(C[n]);
+            const float f[4] = {to_f32(Bm[0]), to_f32(Bm[1]), to_f32(Bm[2]), to_f32(Bm[3])};
+            const float g[4] = {to_f32(C[0]), to_f32(C[1]), to_f32(C[2]), to_f32(C[3])};
+            bq[k] = Vec<E, 4>::pack(f);  // (exact)
+            cq[k] = Vec<E, 4>::pack(g);
         }
     }
     const float4 a = *reinterpret_cast<const float4 *>(p.A + (long long)c * (4 * LPC) + 4 * q);
@@ -506,22 +507,25 @@ __global__ void __launch_bounds__(256) ssm_step_kernel(const __grid_constant__ S
 #pragma unroll
     for (int k = 0; k < kStepSeqs; ++k) {
         const int b = b0 + k;
-        float dt = v[k] + bias;
+        const float uk = to_f32(u[k]);
+        float dt = to_f32(v[k]) + bias;
         if (p.softplus) dt = softplus(dt);
-        const float du = dt * u[k], hv[4] = {h[k].x, h[k].y, h[k].z, h[k].w};
-        float n[4], y = 0.f;
+        const float du = dt * uk, hv[4] = {h[k].x, h[k].y, h[k].z, h[k].w};
+        float n[4], bv[4], cv[4], y = 0.f;
+        Vec<E, 4>::unpack(bq[k], bv);
+        Vec<E, 4>::unpack(cq[k], cv);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            n[j] = fmaf(exp2_hw(dt * av[j]), hv[j], du * bv[k][j]);
-            y = fmaf(cv[k][j], n[j], y);
+            n[j] = fmaf(exp2_hw(dt * av[j]), hv[j], du * bv[j]);
+            y = fmaf(cv[j], n[j], y);
         }
         if (live && b < p.B)
             *reinterpret_cast<float4 *>(p.state + ((long long)b * p.E + c) * (4 * LPC) + 4 * q) = make_float4(n[0], n[1], n[2], n[3]);
 #pragma unroll
         for (int o = LPC / 2; o > 0; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
         if (live && b < p.B && q == 0) {
-            y = fmaf(skip, u[k], y);
-            if (p.z) y *= silu<E>(zv[k]);
+            y = fmaf(skip, uk, y);
+            if (p.z) y *= silu<E>(to_f32(zv[k]));
             static_cast<E *>(p.out)[(long long)b * p.E + c] = from_f32<E>(y);
         }
     }
@@ -693,12 +697,21 @@ template <typename E> cudaError_t ssm_step_e(SsmParams &p, cudaStream_t s) {
     const long long rows = quads ? (p.B + kStepSeqs - 1) / kStepSeqs : p.B;
     if (per * rows > 0x7fffffffLL) return cudaErrorInvalidValue;
     const unsigned ctas = static_cast<unsigned>(per * rows);
+    const bool on4 = (reinterpret_cast<uintptr_t>(p.Bm) | reinterpret_cast<uintptr_t>(p.C)) % (4 * sizeof(E)) == 0 &&
+                     p.b_stride % 4 == 0 && p.c_stride % 4 == 0;
+    auto run = [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value;
+        if (on4)
+            ssm_step_kernel<E, L, true><<<ctas, 256, 0, s>>>(p);
+        else
+            ssm_step_kernel<E, L, false><<<ctas, 256, 0, s>>>(p);
+    };
     switch (lpc) {
-    case 1: ssm_step_kernel<E, 1><<<ctas, 256, 0, s>>>(p); break;
-    case 2: ssm_step_kernel<E, 2><<<ctas, 256, 0, s>>>(p); break;
-    case 4: ssm_step_kernel<E, 4><<<ctas, 256, 0, s>>>(p); break;
-    case 8: ssm_step_kernel<E, 8><<<ctas, 256, 0, s>>>(p); break;
-    case 16: ssm_step_kernel<E, 16><<<ctas, 256, 0, s>>>(p); break;
+    case 1: run(std::integral_constant<int, 1>()); break;
+    case 2: run(std::integral_constant<int, 2>()); break;
+    case 4: run(std::integral_constant<int, 4>()); break;
+    case 8: run(std::integral_constant<int, 8>()); break;
+    case 16: run(std::integral_constant<int, 16>()); break;
     default: ssm_step_any_kernel<E><<<ctas, 128, 0, s>>>(p);
     }
     return cudaGetLastError();

@@ -479,10 +479,10 @@ def _new(given: Optional[torch.Tensor], shape, dtype: torch.dtype, like: torch.T
         if given.get_device() != like.get_device():
             raise ValueError(f"{name} must be on the inputs' device")
         return given
-    if stream is None:
-        return like.new_empty(shape, dtype=dtype)
+    if stream is None:  # (a tensor's new_empty takes twice as long)
+        return torch.empty(shape, dtype=dtype, device=like.device)
     with torch.cuda.stream(stream):
-        return like.new_empty(shape, dtype=dtype)
+        return torch.empty(shape, dtype=dtype, device=like.device)
 
 
 def _row_stride(t: torch.Tensor, name: str) -> int:
