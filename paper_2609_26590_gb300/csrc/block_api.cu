@@ -230,7 +230,7 @@ gtr_status_t gtr_swiglu_ffn_fwd(const void *x, long long x_stride, const void *w
 
 size_t gtr_swiglu_ffn_bwd_workspace_bytes(long long M, int D, int F) {
     if (check_ffn(M, D, F, GTR_F16) != GTR_OK) return 0;
-    return gtr::ffn_bwd_workspace(M, F);
+    return gtr::ffn_bwd_workspace(M, D, F);
 }
 
 gtr_status_t gtr_swiglu_ffn_bwd(const void *dout, long long dout_stride, const void *x, long long x_stride,
@@ -250,7 +250,7 @@ gtr_status_t gtr_swiglu_ffn_bwd(const void *dout, long long dout_stride, const v
     }
     if (!dout || !x || !w_gate || !w_value || !dx || !at16(dout) || !at16(x) || !at16(w_gate) || !at16(w_value) || !at16(dx))
         return GTR_ERR_INVALID_ARG;
-    const size_t need = gtr::ffn_bwd_workspace(M, F);
+    const size_t need = gtr::ffn_bwd_workspace(M, D, F);
     if (workspace == nullptr || workspace_bytes < need) return GTR_ERR_WORKSPACE;
     const Span outs[4] = {rows(dx, M, D, D, 2), rows(dw_gate, F, D, D, 2), rows(dw_value, F, D, D, 2),
                           Span{workspace, static_cast<long long>(need)}};

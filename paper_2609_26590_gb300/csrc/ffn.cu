@@ -3,23 +3,23 @@
 //   dV = dH SiLU(G), dG = dH V s(G) (1 + G (1 - s(G)))          s: the logistic function
 //   dX = dG Wg + dV Wv,  dWg = dG^T X,  dWv = dV^T X
 //
-// Four products of one persistent kernel, which differ in their operands' major-ness and in what
-// happens to the fp32 accumulator on its way out:
-//   kFwd  both projections of 128 channels as one 256-column tile (gate columns from the even CTA's
-//         weights, value columns from the odd one's), SiLU and the product in registers, H stored
-//   kAct  the same projections again (nothing of M x F is kept between the passes), dH read beside
-//         them, dG and dV stored in the inputs' type: they are operands of the next two products,
-//         which the tensor cores take in 16 bits (half a step of rounding each)
-//   kDx   [dG dV] [Wg; Wv], the weights read along F (MN-major)
-//   kDw   dG^T X and dV^T X, both operands read along the tokens (MN-major)
-//
-// A CTA pair (tcgen05 cta_group::2) computes 256 x 256 (128) tiles: 64-deep blocks of both operands
-// arrive by TMA in 128-byte-swizzled shared memory (rows and columns outside the tensors as zeros),
-// one warp issues the MMAs, and eight warps empty one TMEM accumulator while the next tile fills
-// the other.  Every wait is bounded; a kernel that gives up sets the status word.
+// Products of persistent kernels on CTA pairs (tcgen05 cta_group::2): 64-deep blocks of both operands
+// arrive by TMA in 128-byte-swizzled shared memory (rows and columns outside the tensors as zeros), one
+// warp issues the MMAs, and eight warps empty the TMEM accumulator.
+//   ffn_kernel<kFwd>  both projections of 128 channels as one 256 x 256 tile (gate columns from the even CTA's
+//                     weights, value columns from the odd one's), SiLU and the product in registers, H stored; the
+//                     next tile fills a second accumulator meanwhile
+//   ffn_kernel<kAct>  the same projections again (nothing of M x F is kept between the passes), dH read beside
+//                     them, dG and dV stored in the inputs' type: they are operands of the next products,
+//                     which the tensor cores take in 16 bits (half a step of rounding each)
+//   ffn_grad_kernel   dX = [dG dV] [Wg; Wv], the weights read along F (MN-major), and dWg, dWv, both operands read
+//                     along the tokens (MN-major), as one launch whose tiles are dealt so that the pairs end
+//                     together; dW's long sums may be cut between pairs (ffn_grad_plan)
+// Every wait is bounded; a kernel that gives up sets the status word.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cstdint>
 #include <cstring>
@@ -38,7 +38,7 @@ namespace {
 
 using namespace ptx;
 
-enum : int { kFwd = 0, kAct = 1, kDx = 2, kDw = 3 };
+enum : int { kFwd = 0, kAct = 1 };
 
 constexpr int kFfnThreads = 384;   // warps: loads, MMAs, TMEM, idle, eight epilogue warps
 constexpr int kFfnEpiWarp = 4;
@@ -49,21 +49,20 @@ constexpr int kStageBytes = 2 * kStageA;
 constexpr int kBox = 32 * 128;     // an epilogue warp's box: 32 rows x 64 columns of 16 bits
 constexpr uint64_t kFfnWaitNs = 1000000000ull;
 
-constexpr int ffn_stages(int mode) { return mode == kAct ? 5 : 6; }
-constexpr int ffn_boxes(int mode) { return mode == kAct ? 2 : 1; }  // staging boxes of a warp
+constexpr int ffn_stages(int mode) { return mode == kAct ? 4 : 6; }
+constexpr int ffn_boxes(int mode) { return mode == kAct ? 3 : 1; }  // staging boxes of a warp: outputs, dH
 constexpr size_t ffn_smem(int mode) {
     return (size_t)ffn_stages(mode) * kStageBytes + 8 * (size_t)ffn_boxes(mode) * kBox + 1024;
 }
 
 struct FfnParams {
-    CUtensorMap a[2], b[2];  // operands (the second: the odd CTA's weights, or the second half of the product)
-    CUtensorMap o[2];        // outputs
-    CUtensorMap dh;          // kAct
-    FastDiv tm;              // tiles down the rows
+    CUtensorMap a, b[2];  // tokens; gate and value weights
+    CUtensorMap o[2];     // H, or dG and dV
+    CUtensorMap dh;       // kAct
+    FastDiv tm;           // tiles down the rows
     int tiles;
-    int nk, nk_half;         // 64-deep blocks of a tile; of one of kDx's two products
-    int rows, cols;          // extent of an output
-    int bn;                  // columns of a tile's accumulator
+    int nk;               // 64-deep blocks of a tile
+    int rows, cols;       // M, F
     uint32_t idesc;
 };
 
@@ -86,9 +85,12 @@ __device__ __forceinline__ f2 sigmoid2(f2 z) {
     return pack2(r0, r1);
 }
 
+__device__ __forceinline__ uint64_t kmajor_desc(uint32_t saddr) { return smem_desc(saddr, 16, 1024, kLayoutSw128); }
+// 64 x 64 blocks, 8 KB apart along M or N
+__device__ __forceinline__ uint64_t mnmajor_desc(uint32_t saddr) { return smem_desc(saddr, 8192, 1024, kLayoutSw128); }
+
 template <int MODE, typename E>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_constant__ FfnParams p) {
-    constexpr bool A_MN = MODE == kDw, B_MN = MODE == kDx || MODE == kDw;
     constexpr int S = ffn_stages(MODE), BOXES = ffn_boxes(MODE);
     extern __shared__ uint8_t ffn_raw[];
     __shared__ FfnBars bars;
@@ -125,8 +127,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
     if (warp == 0) {
         if (lane == 0) {
             // ---- loads: this CTA's half of A's rows and of B's columns, counted on the even CTA's barrier
-            const int bhalf = p.bn / 2;
-            const uint32_t bytes = 2u * (kStageA + static_cast<uint32_t>(bhalf) * 128u);
+            constexpr uint32_t bytes = 2u * kStageBytes;
             uint32_t it = 0;
             bool ok = true;
             for (int tile = pair; ok && tile < p.tiles; tile += pairs) {
@@ -141,21 +142,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
                     const uint32_t bar = map_to_cta(smem_u32(&bars.full[s]), 0);
                     if (rank == 0) mbar_arrive_expect_tx(&bars.full[s], bytes);
                     const uint32_t sa = smem_u32(smem) + s * kStageBytes, sb = sa + kStageA;
-                    if constexpr (MODE == kFwd || MODE == kAct) {
-                        tma_load_2d_pair(sa, &p.a[0], bar, k * kBlockK, m * kTileM + rank * 128);
-                        tma_load_2d_pair(sb, &p.b[rank], bar, k * kBlockK, n * 128);
-                    } else if constexpr (MODE == kDx) {
-                        const int half = k >= p.nk_half, kk = (k - half * p.nk_half) * kBlockK;
-                        tma_load_2d_pair(sa, &p.a[half], bar, kk, m * kTileM + rank * 128);
-                        for (int j = 0; j < bhalf; j += 64)
-                            tma_load_2d_pair(sb + j * 128, &p.b[half], bar, n * p.bn + rank * bhalf + j, kk);
-                    } else {
-                        const int mt = p.tm.d / 2, g = m >= mt, m0 = (m - g * mt) * kTileM + rank * 128;
-                        for (int j = 0; j < 128; j += 64)
-                            tma_load_2d_pair(sa + j * 128, &p.a[g], bar, m0 + j, k * kBlockK);
-                        for (int j = 0; j < bhalf; j += 64)
-                            tma_load_2d_pair(sb + j * 128, &p.b[0], bar, n * p.bn + rank * bhalf + j, k * kBlockK);
-                    }
+                    tma_load_2d_pair(sa, &p.a, bar, k * kBlockK, m * kTileM + rank * 128);
+                    tma_load_2d_pair(sb, &p.b[rank], bar, k * kBlockK, n * 128);
                 }
             }
             // every block consumed: no copy and no barrier arrival is in flight any more
@@ -180,9 +168,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t sa = smem_u32(smem) + s * kStageBytes, sb = sa + kStageA;
-                    const uint64_t ad = smem_desc(sa, A_MN ? 8192 : 16, 1024, kLayoutSw128);
-                    const uint64_t bd = smem_desc(sb, B_MN ? 8192 : 16, 1024, kLayoutSw128);
-                    mma4_f16_ss_pair<A_MN ? 128 : 2, B_MN ? 128 : 2>(tmem + buf * 256, ad, bd, p.idesc, k > 0);
+                    mma4_f16_ss_pair<2, 2>(tmem + buf * 256, kmajor_desc(sa), kmajor_desc(sb), p.idesc, k > 0);
                     mma_commit_pair(&bars.empty[s]);
                 }
                 if (ok) mma_commit_pair(&bars.acc_full[buf]);
@@ -195,23 +181,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
         uint8_t *box = smem + S * kStageBytes + (size_t)w * BOXES * kBox;
         const uint32_t lanes = static_cast<uint32_t>(sub * 32) << 16;
         const uint32_t acc_empty = map_to_cta(smem_u32(&bars.acc_empty[0]), 0);  // the even CTA's, 8 bytes apart
+        // dH of the next tile arrives while this one's outputs are stored and its accumulator is filled
+        auto load_dh = [&](int tile) {
+            if (tile >= p.tiles) return;
+            const int n = fdiv(tile, p.tm), m = tile - n * p.tm.d;
+            mbar_arrive_expect_tx(&bars.dh[w], kBox);
+            tma_load_2d(box + 2 * kBox, &p.dh, &bars.dh[w], n * 128 + half * 64,
+                        m * kTileM + static_cast<int>(rank) * 128 + sub * 32);
+        };
+        if constexpr (MODE == kAct) {
+            if (lane == 0) load_dh(pair);
+        }
         uint32_t acc = 0;
         for (int tile = pair; tile < p.tiles; tile += pairs, ++acc) {
             const int n = fdiv(tile, p.tm), m = tile - n * p.tm.d;
             const uint32_t buf = acc & 1;
-            int row0 = m * kTileM + static_cast<int>(rank) * 128 + sub * 32, group = 0;
-            if constexpr (MODE == kDw) {
-                const int mt = p.tm.d / 2;
-                group = m >= mt;
-                row0 -= group * mt * kTileM;
-            }
-            if constexpr (MODE == kAct) {
-                if (lane == 0) {
-                    bulk_wait_read();  // the box of the tile before has been stored
-                    mbar_arrive_expect_tx(&bars.dh[w], kBox);
-                    tma_load_2d(box, &p.dh, &bars.dh[w], n * 128 + half * 64, row0);
-                }
-            }
+            const int row0 = m * kTileM + static_cast<int>(rank) * 128 + sub * 32;
             bool ok = mbar_wait(&bars.acc_full[buf], (acc >> 1) & 1, abort, kFfnWaitNs);
             if constexpr (MODE == kAct) ok = mbar_wait(&bars.dh[w], acc & 1, nullptr, kFfnWaitNs) && ok;
             if (!__all_sync(0xffffffffu, ok)) {
@@ -220,11 +205,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
             }
             tc_fence_after();
             const uint32_t taddr = tmem + buf * 256 + lanes;
-            if constexpr (MODE == kFwd || MODE == kAct) {
-                if (MODE == kFwd) {
-                    if (lane == 0) bulk_wait_read();
-                    __syncwarp();
-                }
+            {
+                if (lane == 0) bulk_wait_read();  // the boxes of the tile before have been stored
+                __syncwarp();
                 const int col0 = n * 128 + half * 64;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -242,7 +225,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
                         uint4 *at = reinterpret_cast<uint4 *>(box + lane * 128 + (((c * 4 + j) ^ (lane & 7)) << 4));
                         uint32_t in[4], o0[4], o1[4];
                         if constexpr (MODE == kAct) {
-                            const uint4 d = *at;
+                            const uint4 d = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint8_t *>(at) + 2 * kBox);
                             in[0] = d.x, in[1] = d.y, in[2] = d.z, in[3] = d.w;
                         }
 #pragma unroll
@@ -269,41 +252,270 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0 && row0 < p.rows && col0 < p.cols) {
-                    tma_store_2d(&p.o[0], box, col0, row0);
-                    if constexpr (MODE == kAct) tma_store_2d(&p.o[1], box + kBox, col0, row0);
-                    bulk_commit();
+                if (lane == 0) {
+                    if constexpr (MODE == kAct) load_dh(tile + pairs);
+                    if (row0 < p.rows && col0 < p.cols) {
+                        tma_store_2d(&p.o[0], box, col0, row0);
+                        if constexpr (MODE == kAct) tma_store_2d(&p.o[1], box + kBox, col0, row0);
+                        bulk_commit();
+                    }
                 }
-            } else {
-                const int width = p.bn / 2;
+            }
+        }
+        if constexpr (MODE == kAct) {  // after giving up: the last dH box may still be on its way
+            if (lane == 0 && pair + static_cast<int>(acc) * pairs < p.tiles) mbar_wait(&bars.dh[w], acc & 1, nullptr, kFfnWaitNs);
+        }
+        if (lane == 0) bulk_wait_all();
+    }
+    __syncwarp();  // the barriers below are the whole warp's
+    tc_fence_before();
+    __syncthreads();
+    __syncwarp();
+    cluster_sync();  // neither CTA leaves while the other may still signal it or use its TMEM
+    tc_fence_after();
+    if (warp == 2) tmem_dealloc_pair(tmem, 512);
+}
+
+// ---------------------------------------------------------------- dX, dWg and dWv
+constexpr int kGradMaxPairs = 128;
+constexpr int kGradSmem = 227 * 1024 - 2048;        // operand stages and the epilogue's boxes
+constexpr int kGradMinCut = 8;                      // blocks of K that a cut of dW's sums leaves at least
+
+struct GradParams {
+    CUtensorMap ax[2], bx[2];  // dX: dG, dV by tokens; Wg, Wv by F
+    CUtensorMap aw[2], bw;     // dW: dG, dV and the tokens, by tokens (MN-major)
+    CUtensorMap o[3];          // dX, dWg, dWv
+    FastDiv x_tm, w_tm, w_nk;  // tiles down dX's rows and down both dW's; 64-deep blocks of a dW tile
+    int x_tiles, x_nk, x_half; // dX's tiles, blocks of one, blocks of its first product
+    int n_cols, stages;        // accumulator columns: a multiple of 128 up to 512
+    int M, D, F;
+    uint32_t x_idesc[2], w_idesc[2];  // of the first 256 columns and of the rest
+    float *partial;                   // [2 pairs] tiles of cut sums, [n_cols / 4][256][4] each
+    int w_start[kGradMaxPairs + 1];   // a pair's blocks of dW: its share of w_tiles x w_nk
+};
+
+struct GradBars {
+    uint64_t full[8], empty[8], acc_full, acc_empty[2];
+    uint32_t tmem, abort;
+};
+
+// One tile, or one stretch of a dW tile's sum.
+struct GradItem {
+    bool w;      // dW
+    int m, n, g; // tile; dWg or dWv
+    int k0, k1;
+    int slot;    // of a cut sum, else -1
+};
+// A pair's items in order: its dX tiles, then its stretch of dW.  Every role walks them alike.
+struct GradWalk {
+    int tile, pos, end, pair;
+    __device__ __forceinline__ GradWalk(const GradParams &p, int pair_)
+        : tile(pair_), pos(p.w_start[pair_]), end(p.w_start[pair_ + 1]), pair(pair_) {}
+    __device__ __forceinline__ bool next(const GradParams &p, int pairs, GradItem *it) {
+        it->g = 0;
+        it->slot = -1;
+        if (tile < p.x_tiles) {
+            it->w = false;
+            it->n = fdiv(tile, p.x_tm);
+            it->m = tile - it->n * p.x_tm.d;
+            it->k0 = 0;
+            it->k1 = p.x_nk;
+            tile += pairs;
+            return true;
+        }
+        if (pos >= end) return false;
+        it->w = true;
+        const int t = fdiv(pos, p.w_nk), nk = p.w_nk.d;
+        it->k0 = pos - t * nk;
+        it->k1 = end - pos < nk - it->k0 ? it->k0 + end - pos : nk;
+        pos += it->k1 - it->k0;
+        if (it->k1 - it->k0 < nk) it->slot = 2 * pair + (it->k0 == 0);
+        it->n = fdiv(t, p.w_tm);
+        it->m = t - it->n * p.w_tm.d;
+        const int half = p.w_tm.d / 2;
+        it->g = it->m >= half;
+        it->m -= it->g * half;
+        return true;
+    }
+};
+
+template <typename E>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_grad_kernel(const __grid_constant__ GradParams p) {
+    extern __shared__ uint8_t ffn_raw[];
+    __shared__ GradBars bars;
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(ffn_raw) + 1023) & ~uintptr_t(1023));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, S = p.stages;
+    volatile uint32_t *abort = &bars.abort;
+    // columns in the two MMAs of a block, and what this CTA stages of them (64-column blocks of 8 KB)
+    const int n1 = p.n_cols < 256 ? p.n_cols : 256, n2 = p.n_cols - n1, blocks1 = n1 / 128, blocks = p.n_cols / 128;
+    const uint32_t stage_bytes = kStageA + 8192u * blocks;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S; ++i) mbar_init(&bars.full[i], 1), mbar_init(&bars.empty[i], 1);
+        mbar_init(&bars.acc_full, 1);
+        for (int i = 0; i < 2; ++i) mbar_init(&bars.acc_empty[i], 16);
+        bars.abort = 0;
+        fence_mbar_init();
+    }
+    if (warp == 2) {
+        tmem_alloc_pair(&bars.tmem, 512);
+        tmem_relinquish_pair();
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    __syncwarp();
+    cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem = bars.tmem;
+
+    auto give_up = [&] {
+        *abort = 1;
+        atomicOr(&g_ffn_status, kStatusTimeout);
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0, s = 0, turn = 0;  // blocks so far, their stage, times around the stages
+            bool ok = true;
+            GradWalk walk(p, pair);
+            GradItem item;
+            while (ok && walk.next(p, pairs, &item)) {
+                const int row = item.m * kTileM + rank * 128;
+                for (int k = item.k0; k < item.k1; ++k, ++it) {
+                    if (turn > 0 && !mbar_wait(&bars.empty[s], (turn - 1) & 1, abort, kFfnWaitNs)) {
+                        give_up();
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t bar = map_to_cta(smem_u32(&bars.full[s]), 0);
+                    if (rank == 0) mbar_arrive_expect_tx(&bars.full[s], 2 * stage_bytes);
+                    const uint32_t sa = smem_u32(smem) + s * stage_bytes, sb = sa + kStageA;
+                    const int half = !item.w && k >= p.x_half, kk = (k - half * p.x_half) * kBlockK;
+                    if (!item.w) {
+                        tma_load_2d_pair(sa, &p.ax[half], bar, kk, row);
+                    } else {
+                        tma_load_2d_pair(sa, &p.aw[item.g], bar, row, kk);
+                        tma_load_2d_pair(sa + 8192, &p.aw[item.g], bar, row + 64, kk);
+                    }
+                    const CUtensorMap *b = item.w ? &p.bw : &p.bx[half];
+                    for (int j = 0; j < blocks; ++j) {
+                        const int col = j < blocks1 ? rank * (n1 / 2) + 64 * j : n1 + rank * (n2 / 2) + 64 * (j - blocks1);
+                        tma_load_2d_pair(sb + 8192 * j, b, bar, item.n * p.n_cols + col, kk);
+                    }
+                    if (++s == static_cast<uint32_t>(S)) s = 0, ++turn;
+                }
+            }
+            // every block consumed: no copy and no barrier arrival is in flight any more
+            const uint32_t last = it < static_cast<uint32_t>(S) ? it : S;
+            for (uint32_t i = it - last; i != it; ++i)
+                if (!mbar_wait(&bars.empty[i % S], (i / S) & 1, nullptr, kFfnWaitNs)) give_up();
+        }
+    } else if (warp == 1) {
+        if (rank == 0) {
+            uint32_t s = 0, turn = 0, tile = 0;
+            bool ok = true;
+            GradWalk walk(p, pair);
+            GradItem item;
+            while (ok && walk.next(p, pairs, &item)) {
+                for (int k = item.k0; k < item.k1; ++k) {
+                    ok = __all_sync(0xffffffffu, mbar_wait_cluster(&bars.full[s], turn & 1, abort, kFfnWaitNs));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t sa = smem_u32(smem) + s * stage_bytes, sb = sa + kStageA;
+                    const uint32_t more = k > item.k0;
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        if (part == 1 && n2 == 0) break;
+                        // the first block of a tile waits for the columns of the tile before to be read
+                        if (!more && tile > 0) {
+                            ok = __all_sync(0xffffffffu, mbar_wait_cluster(&bars.acc_empty[part], (tile - 1) & 1, abort, kFfnWaitNs));
+                            if (!ok) break;
+                            tc_fence_after();
+                        }
+                        const uint32_t d = tmem + part * 256, b = sb + part * blocks1 * 8192;
+                        if (item.w)
+                            mma4_f16_ss_pair<128, 128>(d, mnmajor_desc(sa), mnmajor_desc(b), p.w_idesc[part], more);
+                        else
+                            mma4_f16_ss_pair<2, 128>(d, kmajor_desc(sa), mnmajor_desc(b), p.x_idesc[part], more);
+                    }
+                    if (!ok) break;
+                    mma_commit_pair(&bars.empty[s]);
+                    if (++s == static_cast<uint32_t>(S)) s = 0, ++turn;
+                }
+                if (ok) mma_commit_pair(&bars.acc_full);
+                ++tile;
+            }
+            if (!ok && lane == 0) give_up();
+        }
+    } else if (warp >= kFfnEpiWarp) {
+        const int w = warp - kFfnEpiWarp, sub = warp & 3, half = w >> 2;
+        uint8_t *box = smem + S * stage_bytes + (size_t)w * kBox;
+        const uint32_t lanes = static_cast<uint32_t>(sub * 32) << 16;
+        const uint32_t acc_empty = map_to_cta(smem_u32(&bars.acc_empty[0]), 0);  // the even CTA's, 8 bytes apart
+        uint32_t tile = 0;
+        GradWalk walk(p, pair);
+        GradItem item;
+        while (walk.next(p, pairs, &item)) {
+            const bool ok = mbar_wait(&bars.acc_full, tile & 1, abort, kFfnWaitNs);
+            if (!__all_sync(0xffffffffu, ok)) {
+                if (lane == 0) give_up();
+                break;
+            }
+            ++tile;
+            tc_fence_after();
+            const int row0 = item.m * kTileM + static_cast<int>(rank) * 128 + sub * 32;
+            const int rows = item.w ? p.F : p.M;
+            const CUtensorMap *out = &p.o[item.w ? 1 + item.g : 0];
+            float4 *cut = item.slot < 0 ? nullptr
+                                        : reinterpret_cast<float4 *>(p.partial) + (size_t)item.slot * (p.n_cols / 4) * kTileM +
+                                              rank * 128 + sub * 32 + lane;
+#pragma unroll 1
+            for (int part = 0; part < 2; ++part) {
+                const int width = (part == 0 ? n1 : n2) / 2;
+                if (width == 0) break;
                 for (int b0 = 0; b0 < width; b0 += 64) {
-                    const int off = half * width + b0, col0 = n * p.bn + off;
-                    if (lane == 0) bulk_wait_read();
-                    __syncwarp();
+                    const int off = part * 256 + half * width + b0, col0 = item.n * p.n_cols + off;
+                    if (cut == nullptr) {
+                        if (lane == 0) bulk_wait_read();
+                        __syncwarp();
+                    }
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         uint32_t g[32];
-                        tmem_ld_32x32(taddr + off + c * 32, g);
+                        tmem_ld_32x32(tmem + lanes + off + c * 32, g);
                         tmem_ld_wait();
                         if (c == 1 && b0 + 64 >= width) {
                             tc_fence_before();
                             __syncwarp();
-                            if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty + 8 * buf);
+                            if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty + 8 * part);
                         }
+                        if (cut != nullptr) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            float o0[8];
+                            for (int j = 0; j < 8; ++j)
+                                cut[(size_t)((off + c * 32) / 4 + j) * kTileM] =
+                                    make_float4(__uint_as_float(g[4 * j]), __uint_as_float(g[4 * j + 1]),
+                                                __uint_as_float(g[4 * j + 2]), __uint_as_float(g[4 * j + 3]));
+                        } else {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) o0[i] = __uint_as_float(g[8 * j + i]);
-                            *reinterpret_cast<uint4 *>(box + lane * 128 + (((c * 4 + j) ^ (lane & 7)) << 4)) =
-                                Vec<E, 8>::pack(o0);
+                            for (int j = 0; j < 4; ++j) {
+                                float o[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) o[i] = __uint_as_float(g[8 * j + i]);
+                                *reinterpret_cast<uint4 *>(box + lane * 128 + (((c * 4 + j) ^ (lane & 7)) << 4)) =
+                                    Vec<E, 8>::pack(o);
+                            }
                         }
                     }
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0 && row0 < p.rows && col0 < p.cols) {
-                        tma_store_2d(&p.o[group], box, col0, row0);
-                        bulk_commit();
+                    if (cut == nullptr) {
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0 && row0 < rows && col0 < p.D) {
+                            tma_store_2d(out, box, col0, row0);
+                            bulk_commit();
+                        }
                     }
                 }
             }
@@ -317,6 +529,53 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
     cluster_sync();  // neither CTA leaves while the other may still signal it or use its TMEM
     tc_fence_after();
     if (warp == 2) tmem_dealloc_pair(tmem, 512);
+}
+
+// Sums of dW tiles that were cut between pairs, in the order of K, rounded once.  A CTA takes 32 columns of
+// a tile, a thread one of its 256 rows.
+struct GradSumParams {
+    const float *partial;
+    void *dw[2];
+    FastDiv w_tm;
+    int nk, pairs, n_cols, D, F;
+    int w_start[kGradMaxPairs + 1];
+};
+template <typename E> __global__ void __launch_bounds__(kTileM) ffn_grad_sum_kernel(const __grid_constant__ GradSumParams p) {
+    const int t = blockIdx.y, row = threadIdx.x, c = blockIdx.x * 8;  // c: first group of four columns
+    const int first = t * p.nk, last = first + p.nk;
+    int lo = 0, hi = p.pairs - 1;  // the pair that holds the tile's first block
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (p.w_start[mid] <= first)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    if (p.w_start[lo] <= first && p.w_start[lo + 1] >= last) return;  // a whole tile: stored by its pair
+    float4 sum[8] = {};
+    for (int pair = lo; pair < p.pairs && p.w_start[pair] < last; ++pair) {
+        if (p.w_start[pair + 1] <= p.w_start[pair] || p.w_start[pair + 1] <= first) continue;
+        const int slot = 2 * pair + (p.w_start[pair] <= first);
+        const float4 *src = reinterpret_cast<const float4 *>(p.partial) + (size_t)slot * (p.n_cols / 4) * kTileM + row;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float4 v = src[(size_t)(c + j) * kTileM];
+            sum[j].x += v.x, sum[j].y += v.y, sum[j].z += v.z, sum[j].w += v.w;
+        }
+    }
+    const int n = fdiv(t, p.w_tm);
+    int m = t - n * p.w_tm.d;
+    const int half = p.w_tm.d / 2, g = m >= half;
+    m -= g * half;
+    const int r = m * kTileM + row;
+    if (r >= p.F) return;
+    E *out = static_cast<E *>(p.dw[g]) + (size_t)r * p.D;
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+        const int col = n * p.n_cols + 4 * (c + j);
+        const float f[8] = {sum[j].x, sum[j].y, sum[j].z, sum[j].w, sum[j + 1].x, sum[j + 1].y, sum[j + 1].z, sum[j + 1].w};
+        if (col < p.D) st_vec<E, 8>(out + col, f);  // (D is a multiple of 8)
+    }
 }
 
 // A row-major matrix [rows][cols] of 16-bit elements at `stride` elements a row, in boxes of 64 columns
@@ -363,81 +622,203 @@ bool set_tiles(FfnParams &p, int tm, int tn) {
     return true;
 }
 
-// Columns of the kDx and kDw tiles: 128 wastes fewer columns behind D, 256 reads each A block half as often.
-int tile_columns(int D) { return D % 256 == 0 || D > 1024 ? 256 : 128; }
+
+// How dX's and dW's tiles are dealt to the pairs.
+struct GradPlan {
+    int pairs, n_cols;
+    int x_tm, x_tiles, x_nk, w_tm, w_tiles, w_nk;
+    bool cut;                        // some dW tile's sum is cut between pairs
+    int w_start[kGradMaxPairs + 1];
+};
+
+// Whole tiles (dX's dealt round, then each dW tile to the pair that is least loaded), or dW's blocks of K cut so that
+// all pairs end together, whichever costs less; for each tile width.  A block of K takes a pair the longer of its MMAs
+// (two cycles a column) and of its operands' way into shared memory (50 bytes a cycle and SM was measured, which is what
+// bounds 256 x 256 tiles at about 85 % of the tensor cores' rate; wider ones read A less often), a tile's epilogue
+// about 4,000 cycles, and a cut sum's partial tiles their way to memory and back.
+bool ffn_grad_plan(long long M, int D, int F, int n_sm, GradPlan *out) {
+    GradPlan g;
+    g.pairs = n_sm / 2 < kGradMaxPairs ? n_sm / 2 : kGradMaxPairs;
+    if (g.pairs < 1) return false;
+    g.x_nk = 2 * ceil_div(F, kBlockK);
+    g.w_nk = ceil_div(M, kBlockK);
+    double least = 0;
+    bool found = false;
+    for (int n = 128; n <= 512; n += 128) {
+        if (n > 128 && n >= D + 128) break;
+        const int tn = ceil_div(D, n);
+        const long long xt = (long long)ceil_div(M, kTileM) * tn, wt = 2LL * ceil_div(F, kTileM) * tn;
+        if (xt > (1 << 29) || wt > (1 << 29) || wt * g.w_nk > (1LL << 30)) continue;
+        g.n_cols = n;
+        g.x_tm = ceil_div(M, kTileM), g.x_tiles = static_cast<int>(xt);
+        g.w_tm = 2 * ceil_div(F, kTileM), g.w_tiles = static_cast<int>(wt);
+        const double mma = 2.0 * n, way = (16384 + 64.0 * n) / 50, block = mma > way ? mma : way;
+        const double x_cost = g.x_nk * block + 4000, w_cost = g.w_nk * block + 4000;
+        const int q = g.x_tiles / g.pairs, r = g.x_tiles % g.pairs;
+        // Whole tiles: the first r pairs have a dX tile more.  Each turn gives one dW tile to every pair of the group that
+        // is less loaded (most turns are skipped at once: both groups get `base`).
+        const int size[2] = {r, g.pairs - r};
+        const double own[2] = {(q + 1) * x_cost, q * x_cost};
+        const int base = g.w_tiles / g.pairs > 64 ? g.w_tiles / g.pairs - 64 : 0;
+        int count[2] = {base, base}, extra[2] = {0, 0};
+        for (int left = g.w_tiles - base * g.pairs; left > 0;) {
+            const int at = size[0] > 0 && own[0] + count[0] * w_cost < own[1] + count[1] * w_cost ? 0 : 1;
+            if (left >= size[at])
+                ++count[at];
+            else
+                extra[at] = left;
+            left -= size[at];
+        }
+        double whole = 0;
+        for (int i = 0; i < 2; ++i)
+            if (size[i] > 0) whole = std::max(whole, own[i] + (count[i] + (extra[i] > 0)) * w_cost);
+        if (!found || whole < least) {
+            found = true;
+            least = whole;
+            g.cut = false;
+            g.w_start[0] = 0;
+            for (int i = 0; i < g.pairs; ++i) {
+                const int at = i < r ? 0 : 1, rank = i < r ? i : i - r;
+                g.w_start[i + 1] = g.w_start[i] + (count[at] + (rank < extra[at])) * g.w_nk;
+            }
+            *out = g;
+        }
+        // cut sums: an even share of the blocks for every pair, after its dX tiles
+        const long long blocks = (long long)g.w_tiles * g.w_nk;
+        double share = (blocks * block + g.x_tiles * x_cost) / g.pairs;  // all pairs' end, if none has too much already
+        if (share < (q + 1) * x_cost && r > 0 && r < g.pairs)
+            share = q * x_cost + blocks * block / (g.pairs - r);  // the pairs with one dX tile more take none
+        const double tiles = std::min(g.pairs + g.w_tiles, 2 * g.pairs);
+        // partial tiles written and read at about 20 bytes a cycle and SM, the sum's launch and tail
+        const double cost = std::max(share, r > 0 ? own[0] : 0.0) + 2 * tiles * kTileM * n * 4.0 / (20.0 * n_sm) + 16000;
+        if (cost < least && g.w_nk >= 4 * kGradMinCut && g.w_tiles <= 65535) {
+            least = cost;
+            g.cut = true;
+            double at = 0;
+            g.w_start[0] = 0;
+            for (int i = 0; i < g.pairs; ++i) {
+                const double left = share - (q + (i < r)) * x_cost;
+                if (left > 0) at += left / block;
+                long long e = static_cast<long long>(at + 0.5);
+                const int k = static_cast<int>(e % g.w_nk);  // no stretch shorter than kGradMinCut at a tile's ends
+                if (k < kGradMinCut)
+                    e -= k;
+                else if (g.w_nk - k < kGradMinCut)
+                    e += g.w_nk - k;
+                if (e > blocks || i + 1 == g.pairs) e = blocks;
+                if (e < g.w_start[i]) e = g.w_start[i];
+                g.w_start[i + 1] = static_cast<int>(e);
+            }
+            *out = g;
+        }
+    }
+    return found;
+}
+size_t grad_partial_bytes(const GradPlan &g) {
+    return g.cut ? (size_t)2 * g.pairs * kTileM * g.n_cols * sizeof(float) : 0;
+}
+size_t act_bytes(long long M, int F) { return ((size_t)M * F * 2 + 255) / 256 * 256; }
+
+template <typename E> cudaError_t grad_launch(const GradParams &p, const GradPlan &g, void *dw_gate, void *dw_value,
+                                              cudaStream_t stream) {
+    static std::atomic<unsigned long long> set_on_devices(0);
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (!(set_on_devices.load(std::memory_order_relaxed) & bit)) {
+        e = cudaFuncSetAttribute(ffn_grad_kernel<E>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGradSmem);
+        if (e != cudaSuccess) return e;
+        set_on_devices.fetch_or(bit);
+    }
+    ffn_grad_kernel<E><<<2 * g.pairs, kFfnThreads, kGradSmem, stream>>>(p);
+    if ((e = cudaGetLastError()) != cudaSuccess || !g.cut) return e;
+    GradSumParams q;
+    q.partial = p.partial;
+    q.dw[0] = dw_gate, q.dw[1] = dw_value;
+    q.w_tm = p.w_tm;
+    q.nk = g.w_nk, q.pairs = g.pairs, q.n_cols = g.n_cols, q.D = p.D, q.F = p.F;
+    std::memcpy(q.w_start, g.w_start, sizeof(q.w_start));
+    ffn_grad_sum_kernel<E><<<dim3(g.n_cols / 32, g.w_tiles), kTileM, 0, stream>>>(q);
+    return cudaGetLastError();
+}
 
 }  // namespace
 
 bool ffn_supported(const FfnProblem &q) { return (q.dtype == 1 || q.dtype == 2) && tensor_map_encoder() != nullptr; }
 
-cudaError_t launch_ffn(const FfnProblem &q, void *out, cudaStream_t stream) {
-    int n_sm = 0;
-    cudaError_t e = sm_count(&n_sm);
-    if (e != cudaSuccess) return e;
-    FfnParams p;
+namespace {
+
+// What the forward pass and the backward pass's first product share.
+bool ffn_params(const FfnProblem &q, FfnParams &p) {
     std::memset(&p, 0, sizeof(p));
-    if (!ffn_map(&p.a[0], q.x, q.dtype, q.M, q.D, q.x_stride, 128) ||
-        !ffn_map(&p.b[0], q.w_gate, q.dtype, q.F, q.D, q.D, 128) ||
-        !ffn_map(&p.b[1], q.w_value, q.dtype, q.F, q.D, q.D, 128) || !ffn_map(&p.o[0], out, q.dtype, q.M, q.F, q.F, 32) ||
-        !set_tiles(p, ceil_div(q.M, kTileM), ceil_div(q.F, 128)))
-        return cudaErrorInvalidValue;
     p.nk = ceil_div(q.D, kBlockK);
     p.rows = static_cast<int>(q.M);
     p.cols = q.F;
-    p.bn = 256;
     p.idesc = instr_desc(q.dtype == 1 ? kFmtF16 : kFmtBF16, kTileM, 256, 0, 0);
+    return ffn_map(&p.a, q.x, q.dtype, q.M, q.D, q.x_stride, 128) &&
+           ffn_map(&p.b[0], q.w_gate, q.dtype, q.F, q.D, q.D, 128) &&
+           ffn_map(&p.b[1], q.w_value, q.dtype, q.F, q.D, q.D, 128) &&
+           set_tiles(p, ceil_div(q.M, kTileM), ceil_div(q.F, 128));
+}
+
+}  // namespace
+
+cudaError_t launch_ffn(const FfnProblem &q, void *out, cudaStream_t stream) {
+    int n_sm = 0;
+    const cudaError_t e = sm_count(&n_sm);
+    if (e != cudaSuccess) return e;
+    FfnParams p;
+    if (!ffn_params(q, p) || !ffn_map(&p.o[0], out, q.dtype, q.M, q.F, q.F, 32)) return cudaErrorInvalidValue;
     return ffn_launch<kFwd>(p, q.dtype, n_sm, stream);
 }
 
-size_t ffn_bwd_workspace(long long M, int F) { return ((size_t)M * F * 2 + 255) / 256 * 256 * 2; }
+size_t ffn_bwd_workspace(long long M, int D, int F) {
+    int n_sm = 0;
+    GradPlan g;
+    size_t cut = 0;
+    if (sm_count(&n_sm) == cudaSuccess && ffn_grad_plan(M, D, F, n_sm, &g)) cut = grad_partial_bytes(g);
+    return 2 * act_bytes(M, F) + cut;
+}
 
 cudaError_t launch_ffn_bwd(const FfnProblem &q, const void *dout, long long dout_stride, void *dx, void *dw_gate,
                            void *dw_value, void *workspace, cudaStream_t stream) {
     int n_sm = 0;
     cudaError_t e = sm_count(&n_sm);
     if (e != cudaSuccess) return e;
-    char *dg = static_cast<char *>(workspace), *dv = dg + ffn_bwd_workspace(q.M, q.F) / 2;
-    const uint32_t fmt = q.dtype == 1 ? kFmtF16 : kFmtBF16;
+    char *dg = static_cast<char *>(workspace), *dv = dg + act_bytes(q.M, q.F);
     FfnParams p;
-    std::memset(&p, 0, sizeof(p));
-    if (!ffn_map(&p.a[0], q.x, q.dtype, q.M, q.D, q.x_stride, 128) ||
-        !ffn_map(&p.b[0], q.w_gate, q.dtype, q.F, q.D, q.D, 128) ||
-        !ffn_map(&p.b[1], q.w_value, q.dtype, q.F, q.D, q.D, 128) || !ffn_map(&p.o[0], dg, q.dtype, q.M, q.F, q.F, 32) ||
-        !ffn_map(&p.o[1], dv, q.dtype, q.M, q.F, q.F, 32) || !ffn_map(&p.dh, dout, q.dtype, q.M, q.F, dout_stride, 32) ||
-        !set_tiles(p, ceil_div(q.M, kTileM), ceil_div(q.F, 128)))
+    if (!ffn_params(q, p) || !ffn_map(&p.o[0], dg, q.dtype, q.M, q.F, q.F, 32) ||
+        !ffn_map(&p.o[1], dv, q.dtype, q.M, q.F, q.F, 32) || !ffn_map(&p.dh, dout, q.dtype, q.M, q.F, dout_stride, 32))
         return cudaErrorInvalidValue;
-    p.nk = ceil_div(q.D, kBlockK);
-    p.rows = static_cast<int>(q.M);
-    p.cols = q.F;
-    p.bn = 256;
-    p.idesc = instr_desc(fmt, kTileM, 256, 0, 0);
+    GradPlan g;
+    if (!ffn_grad_plan(q.M, q.D, q.F, n_sm, &g)) return cudaErrorInvalidValue;
     if ((e = ffn_launch<kAct>(p, q.dtype, n_sm, stream)) != cudaSuccess) return e;
 
-    const int bn = tile_columns(q.D);
-    std::memset(&p, 0, sizeof(p));
-    if (!ffn_map(&p.a[0], dg, q.dtype, q.M, q.F, q.F, 128) || !ffn_map(&p.a[1], dv, q.dtype, q.M, q.F, q.F, 128) ||
-        !ffn_map(&p.b[0], q.w_gate, q.dtype, q.F, q.D, q.D, 64) || !ffn_map(&p.b[1], q.w_value, q.dtype, q.F, q.D, q.D, 64) ||
-        !ffn_map(&p.o[0], dx, q.dtype, q.M, q.D, q.D, 32) || !set_tiles(p, ceil_div(q.M, kTileM), ceil_div(q.D, bn)))
+    GradParams r;
+    std::memset(&r, 0, sizeof(r));
+    if (!ffn_map(&r.ax[0], dg, q.dtype, q.M, q.F, q.F, 128) || !ffn_map(&r.ax[1], dv, q.dtype, q.M, q.F, q.F, 128) ||
+        !ffn_map(&r.bx[0], q.w_gate, q.dtype, q.F, q.D, q.D, 64) || !ffn_map(&r.bx[1], q.w_value, q.dtype, q.F, q.D, q.D, 64) ||
+        !ffn_map(&r.aw[0], dg, q.dtype, q.M, q.F, q.F, 64) || !ffn_map(&r.aw[1], dv, q.dtype, q.M, q.F, q.F, 64) ||
+        !ffn_map(&r.bw, q.x, q.dtype, q.M, q.D, q.x_stride, 64) || !ffn_map(&r.o[0], dx, q.dtype, q.M, q.D, q.D, 32) ||
+        !ffn_map(&r.o[1], dw_gate, q.dtype, q.F, q.D, q.D, 32) || !ffn_map(&r.o[2], dw_value, q.dtype, q.F, q.D, q.D, 32))
         return cudaErrorInvalidValue;
-    p.nk_half = ceil_div(q.F, kBlockK);
-    p.nk = 2 * p.nk_half;
-    p.rows = static_cast<int>(q.M);
-    p.cols = q.D;
-    p.bn = bn;
-    p.idesc = instr_desc(fmt, kTileM, bn, 0, 1);
-    if ((e = ffn_launch<kDx>(p, q.dtype, n_sm, stream)) != cudaSuccess) return e;
-
-    std::memset(&p, 0, sizeof(p));
-    if (!ffn_map(&p.a[0], dg, q.dtype, q.M, q.F, q.F, 64) || !ffn_map(&p.a[1], dv, q.dtype, q.M, q.F, q.F, 64) ||
-        !ffn_map(&p.b[0], q.x, q.dtype, q.M, q.D, q.x_stride, 64) || !ffn_map(&p.o[0], dw_gate, q.dtype, q.F, q.D, q.D, 32) ||
-        !ffn_map(&p.o[1], dw_value, q.dtype, q.F, q.D, q.D, 32) || !set_tiles(p, 2 * ceil_div(q.F, kTileM), ceil_div(q.D, bn)))
-        return cudaErrorInvalidValue;
-    p.nk = ceil_div(q.M, kBlockK);
-    p.rows = q.F;
-    p.cols = q.D;
-    p.bn = bn;
-    p.idesc = instr_desc(fmt, kTileM, bn, 1, 1);
-    return ffn_launch<kDw>(p, q.dtype, n_sm, stream);
+    r.x_tm = make_fastdiv(g.x_tm);
+    r.w_tm = make_fastdiv(g.w_tm);
+    r.w_nk = make_fastdiv(g.w_nk);
+    r.x_tiles = g.x_tiles, r.x_nk = g.x_nk, r.x_half = g.x_nk / 2;
+    r.n_cols = g.n_cols;
+    const int fit = (kGradSmem - 1024 - 8 * kBox) / (kStageA + 8192 * (g.n_cols / 128));
+    r.stages = fit < 8 ? fit : 8;
+    r.M = static_cast<int>(q.M), r.D = q.D, r.F = q.F;
+    const uint32_t fmt = q.dtype == 1 ? kFmtF16 : kFmtBF16;
+    const int n1 = g.n_cols < 256 ? g.n_cols : 256, n2 = g.n_cols - n1;
+    r.x_idesc[0] = instr_desc(fmt, kTileM, n1, 0, 1), r.x_idesc[1] = instr_desc(fmt, kTileM, n2, 0, 1);
+    r.w_idesc[0] = instr_desc(fmt, kTileM, n1, 1, 1), r.w_idesc[1] = instr_desc(fmt, kTileM, n2, 1, 1);
+    r.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + 2 * act_bytes(q.M, q.F));
+    std::memcpy(r.w_start, g.w_start, sizeof(r.w_start));
+    return q.dtype == 1 ? grad_launch<__half>(r, g, dw_gate, dw_value, stream)
+                        : grad_launch<__nv_bfloat16>(r, g, dw_gate, dw_value, stream);
 }
 
 cudaError_t read_and_clear_ffn_status(unsigned int *status) {

@@ -178,8 +178,8 @@ bool ffn_supported(const FfnProblem &p);
 constexpr int kFfnFewTokens = 8;
 cudaError_t launch_ffn_few(const FfnProblem &p, void *out, cudaStream_t stream);
 cudaError_t launch_ffn(const FfnProblem &p, void *out, cudaStream_t stream);
-// Scratch of the backward pass: dG and dV.
-size_t ffn_bwd_workspace(long long M, int F);
+// Scratch of the backward pass on the current device: dG, dV and the partial tiles of cut sums.
+size_t ffn_bwd_workspace(long long M, int D, int F);
 cudaError_t launch_ffn_bwd(const FfnProblem &p, const void *dout, long long dout_stride, void *dx, void *dw_gate,
                            void *dw_value, void *workspace, cudaStream_t stream);
 // Status word of its bounded waits (kStatusTimeout).
