@@ -40,19 +40,21 @@ using namespace ptx;
 
 enum : int { kFwd = 0, kAct = 1 };
 
-constexpr int kFfnThreads = 384;   // warps: loads, MMAs, TMEM, idle, eight epilogue warps
+constexpr int kFfnThreads = 640;   // warps: loads, MMAs, TMEM, idle, sixteen epilogue warps
+constexpr int kGradThreads = 384;  // the same with eight
 constexpr int kFfnEpiWarp = 4;
 constexpr int kTileM = 256;        // accumulator rows of a CTA pair
 constexpr int kBlockK = 64;        // 128 bytes of an operand row
 constexpr int kStageA = 128 * 128; // bytes of a CTA's half of A, and of B
 constexpr int kStageBytes = 2 * kStageA;
-constexpr int kBox = 32 * 128;     // an epilogue warp's box: 32 rows x 64 columns of 16 bits
+constexpr int kBox = 32 * 64;      // an epilogue warp's box: 32 rows x 32 columns of 16 bits
+constexpr int kGradBox = 32 * 128; // ... x 64 columns
 constexpr uint64_t kFfnWaitNs = 1000000000ull;
 
-constexpr int ffn_stages(int mode) { return mode == kAct ? 4 : 6; }
-constexpr int ffn_boxes(int mode) { return mode == kAct ? 3 : 1; }  // staging boxes of a warp: outputs, dH
+constexpr int ffn_stages(int mode) { return mode == kAct ? 5 : 6; }
+constexpr int ffn_boxes(int mode) { return mode == kAct ? 2 : 1; }  // staging boxes of a warp: H, or dG, and dH, then dV
 constexpr size_t ffn_smem(int mode) {
-    return (size_t)ffn_stages(mode) * kStageBytes + 8 * (size_t)ffn_boxes(mode) * kBox + 1024;
+    return (size_t)ffn_stages(mode) * kStageBytes + 16 * (size_t)ffn_boxes(mode) * kBox + 1024;
 }
 
 struct FfnParams {
@@ -67,7 +69,7 @@ struct FfnParams {
 };
 
 struct FfnBars {
-    uint64_t full[6], empty[6], acc_full[2], acc_empty[2], dh[8];
+    uint64_t full[6], empty[6], acc_full[2], acc_empty[2], dh[16];
     uint32_t tmem, abort;
 };
 
@@ -102,8 +104,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S; ++i) mbar_init(&bars.full[i], 1), mbar_init(&bars.empty[i], 1);
-        for (int i = 0; i < 2; ++i) mbar_init(&bars.acc_full[i], 1), mbar_init(&bars.acc_empty[i], 16);
-        for (int i = 0; i < 8; ++i) mbar_init(&bars.dh[i], 1);
+        for (int i = 0; i < 2; ++i) mbar_init(&bars.acc_full[i], 1), mbar_init(&bars.acc_empty[i], 32);
+        for (int i = 0; i < 16; ++i) mbar_init(&bars.dh[i], 1);
         bars.abort = 0;
         fence_mbar_init();
     }
@@ -176,17 +178,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
             if (!ok && lane == 0) give_up();
         }
     } else if (warp >= kFfnEpiWarp) {
-        // ---- epilogue: rows 32 (warp % 4) .. of this CTA's 128, one half of the columns
-        const int w = warp - kFfnEpiWarp, sub = warp & 3, half = w >> 2;
+        // ---- epilogue: rows 32 (warp % 4) .. of this CTA's 128, a quarter of the 128 channels
+        const int w = warp - kFfnEpiWarp, sub = warp & 3, quarter = w >> 2;
         uint8_t *box = smem + S * kStageBytes + (size_t)w * BOXES * kBox;
         const uint32_t lanes = static_cast<uint32_t>(sub * 32) << 16;
         const uint32_t acc_empty = map_to_cta(smem_u32(&bars.acc_empty[0]), 0);  // the even CTA's, 8 bytes apart
-        // dH of the next tile arrives while this one's outputs are stored and its accumulator is filled
+        // dH of the next tile arrives while its accumulator is filled
         auto load_dh = [&](int tile) {
             if (tile >= p.tiles) return;
             const int n = fdiv(tile, p.tm), m = tile - n * p.tm.d;
             mbar_arrive_expect_tx(&bars.dh[w], kBox);
-            tma_load_2d(box + 2 * kBox, &p.dh, &bars.dh[w], n * 128 + half * 64,
+            tma_load_2d(box + kBox, &p.dh, &bars.dh[w], n * 128 + quarter * 32,
                         m * kTileM + static_cast<int>(rank) * 128 + sub * 32);
         };
         if constexpr (MODE == kAct) {
@@ -196,7 +198,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
         for (int tile = pair; tile < p.tiles; tile += pairs, ++acc) {
             const int n = fdiv(tile, p.tm), m = tile - n * p.tm.d;
             const uint32_t buf = acc & 1;
-            const int row0 = m * kTileM + static_cast<int>(rank) * 128 + sub * 32;
+            const int row0 = m * kTileM + static_cast<int>(rank) * 128 + sub * 32, col0 = n * 128 + quarter * 32;
             bool ok = mbar_wait(&bars.acc_full[buf], (acc >> 1) & 1, abort, kFfnWaitNs);
             if constexpr (MODE == kAct) ok = mbar_wait(&bars.dh[w], acc & 1, nullptr, kFfnWaitNs) && ok;
             if (!__all_sync(0xffffffffu, ok)) {
@@ -204,63 +206,61 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
                 break;
             }
             tc_fence_after();
-            const uint32_t taddr = tmem + buf * 256 + lanes;
-            {
-                if (lane == 0) bulk_wait_read();  // the boxes of the tile before have been stored
-                __syncwarp();
-                const int col0 = n * 128 + half * 64;
+            const uint32_t taddr = tmem + buf * 256 + lanes + quarter * 32;
+            uint32_t g[32], v[32];
+            tmem_ld_32x32(taddr, g);
+            tmem_ld_32x32(taddr + 128, v);
+            tmem_ld_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive_cluster_relaxed(acc_empty + 8 * buf);  // the accumulator is in registers
+                if (MODE == kFwd) bulk_wait_read();                // the box of the tile before has been stored
+            }
+            if (MODE == kFwd) __syncwarp();
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t g[32], v[32];
-                    tmem_ld_32x32(taddr + half * 64 + c * 32, g);
-                    tmem_ld_32x32(taddr + 128 + half * 64 + c * 32, v);
-                    tmem_ld_wait();
-                    if (c == 1) {  // the accumulator is in registers
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty + 8 * buf);
-                    }
+            for (int j = 0; j < 4; ++j) {  // 16 bytes: eight columns; 64-byte swizzle
+                uint4 *at = reinterpret_cast<uint4 *>(box + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4));
+                uint4 *at_dh = reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(at) + kBox);
+                uint32_t in[4], o0[4], o1[4];
+                if constexpr (MODE == kAct) {
+                    const uint4 d = *at_dh;
+                    in[0] = d.x, in[1] = d.y, in[2] = d.z, in[3] = d.w;
+                }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {  // 16 bytes: eight columns
-                        uint4 *at = reinterpret_cast<uint4 *>(box + lane * 128 + (((c * 4 + j) ^ (lane & 7)) << 4));
-                        uint32_t in[4], o0[4], o1[4];
-                        if constexpr (MODE == kAct) {
-                            const uint4 d = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint8_t *>(at) + 2 * kBox);
-                            in[0] = d.x, in[1] = d.y, in[2] = d.z, in[3] = d.w;
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const f2 z = pack2(g[8 * j + 2 * i], g[8 * j + 2 * i + 1]);
-                            const f2 y = pack2(v[8 * j + 2 * i], v[8 * j + 2 * i + 1]), sg = sigmoid2(z);
-                            if constexpr (MODE == kFwd) {
-                                const float2 h = unpack2(mul2(mul2(z, sg), y));
-                                o0[i] = pack16<E>(h.x, h.y);
-                            } else {
-                                const float2 d = unpack16<E>(in[i]);
-                                const f2 one = pack2(1.f, 1.f), ds = mul2(pack2(d.x, d.y), sg);
-                                // dG = dH V s (1 + G (1 - s)), dV = dH s G
-                                const float2 dg = unpack2(mul2(mul2(ds, y), fma2(z, fma2(sg, pack2(-1.f, -1.f), one), one)));
-                                const float2 dv = unpack2(mul2(ds, z));
-                                o0[i] = pack16<E>(dg.x, dg.y);
-                                o1[i] = pack16<E>(dv.x, dv.y);
-                            }
-                        }
-                        *at = make_uint4(o0[0], o0[1], o0[2], o0[3]);
-                        if constexpr (MODE == kAct)
-                            *reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(at) + kBox) = make_uint4(o1[0], o1[1], o1[2], o1[3]);
+                for (int i = 0; i < 4; ++i) {
+                    const f2 z = pack2(g[8 * j + 2 * i], g[8 * j + 2 * i + 1]);
+                    const f2 y = pack2(v[8 * j + 2 * i], v[8 * j + 2 * i + 1]), sg = sigmoid2(z);
+                    if constexpr (MODE == kFwd) {
+                        const float2 h = unpack2(mul2(mul2(z, sg), y));
+                        o0[i] = pack16<E>(h.x, h.y);
+                    } else {
+                        const float2 d = unpack16<E>(in[i]);
+                        const f2 one = pack2(1.f, 1.f), ds = mul2(pack2(d.x, d.y), sg);
+                        // dG = dH V s (1 + G (1 - s)), dV = dH s G
+                        const float2 dg = unpack2(mul2(mul2(ds, y), fma2(z, fma2(sg, pack2(-1.f, -1.f), one), one)));
+                        const float2 dv = unpack2(mul2(ds, z));
+                        o0[i] = pack16<E>(dg.x, dg.y);
+                        o1[i] = pack16<E>(dv.x, dv.y);
                     }
                 }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    if constexpr (MODE == kAct) load_dh(tile + pairs);
-                    if (row0 < p.rows && col0 < p.cols) {
-                        tma_store_2d(&p.o[0], box, col0, row0);
-                        if constexpr (MODE == kAct) tma_store_2d(&p.o[1], box + kBox, col0, row0);
-                        bulk_commit();
-                    }
+                *at = make_uint4(o0[0], o0[1], o0[2], o0[3]);
+                if constexpr (MODE == kAct) *at_dh = make_uint4(o1[0], o1[1], o1[2], o1[3]);  // dV where dH was
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                if (row0 < p.rows && col0 < p.cols) {
+                    tma_store_2d(&p.o[0], box, col0, row0);
+                    if constexpr (MODE == kAct) tma_store_2d(&p.o[1], box + kBox, col0, row0);
+                    bulk_commit();
+                }
+                if constexpr (MODE == kAct) {
+                    bulk_wait_read();  // both boxes have been stored: the next dH may come
+                    load_dh(tile + pairs);
                 }
             }
+            __syncwarp();
         }
         if constexpr (MODE == kAct) {  // after giving up: the last dH box may still be on its way
             if (lane == 0 && pair + static_cast<int>(acc) * pairs < p.tiles) mbar_wait(&bars.dh[w], acc & 1, nullptr, kFfnWaitNs);
@@ -340,7 +340,7 @@ struct GradWalk {
 };
 
 template <typename E>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_grad_kernel(const __grid_constant__ GradParams p) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGradThreads, 1) ffn_grad_kernel(const __grid_constant__ GradParams p) {
     extern __shared__ uint8_t ffn_raw[];
     __shared__ GradBars bars;
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(ffn_raw) + 1023) & ~uintptr_t(1023));
@@ -452,7 +452,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
         }
     } else if (warp >= kFfnEpiWarp) {
         const int w = warp - kFfnEpiWarp, sub = warp & 3, half = w >> 2;
-        uint8_t *box = smem + S * stage_bytes + (size_t)w * kBox;
+        uint8_t *box = smem + S * stage_bytes + (size_t)w * kGradBox;
         const uint32_t lanes = static_cast<uint32_t>(sub * 32) << 16;
         const uint32_t acc_empty = map_to_cta(smem_u32(&bars.acc_empty[0]), 0);  // the even CTA's, 8 bytes apart
         uint32_t tile = 0;
@@ -531,7 +531,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
     if (warp == 2) tmem_dealloc_pair(tmem, 512);
 }
 
-// Sums of dW tiles that were cut between pairs, in the order of K, rounded once.  A CTA takes 32 columns of
+// Sums of dW tiles that were cut between pairs, in the order of K, rounded once.  A CTA takes eight columns of
 // a tile, a thread one of its 256 rows.
 struct GradSumParams {
     const float *partial;
@@ -541,7 +541,7 @@ struct GradSumParams {
     int w_start[kGradMaxPairs + 1];
 };
 template <typename E> __global__ void __launch_bounds__(kTileM) ffn_grad_sum_kernel(const __grid_constant__ GradSumParams p) {
-    const int t = blockIdx.y, row = threadIdx.x, c = blockIdx.x * 8;  // c: first group of four columns
+    const int t = blockIdx.y, row = threadIdx.x, c = blockIdx.x * 2;  // c: first group of four columns
     const int first = t * p.nk, last = first + p.nk;
     int lo = 0, hi = p.pairs - 1;  // the pair that holds the tile's first block
     while (lo < hi) {
@@ -551,44 +551,49 @@ template <typename E> __global__ void __launch_bounds__(kTileM) ffn_grad_sum_ker
         else
             hi = mid - 1;
     }
-    if (p.w_start[lo] <= first && p.w_start[lo + 1] >= last) return;  // a whole tile: stored by its pair
-    float4 sum[8] = {};
-    for (int pair = lo; pair < p.pairs && p.w_start[pair] < last; ++pair) {
-        if (p.w_start[pair + 1] <= p.w_start[pair] || p.w_start[pair + 1] <= first) continue;
+    if (p.w_start[lo + 1] >= last) return;  // a whole tile: stored by its pair
+    float f[8] = {};
+    auto source = [&](int pair) {  // a pair's stretch, null when it has none of this tile
+        if (p.w_start[pair + 1] <= p.w_start[pair]) return static_cast<const float4 *>(nullptr);
         const int slot = 2 * pair + (p.w_start[pair] <= first);
-        const float4 *src = reinterpret_cast<const float4 *>(p.partial) + (size_t)slot * (p.n_cols / 4) * kTileM + row;
+        return reinterpret_cast<const float4 *>(p.partial) + ((size_t)slot * (p.n_cols / 4) + c) * kTileM + row;
+    };
+    int end = lo + 1;
+    while (end < p.pairs && p.w_start[end] < last) ++end;
+    for (int pair = lo; pair < end; pair += 4) {  // four stretches' loads together, added in order
+        float4 v[4][2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float4 v = src[(size_t)(c + j) * kTileM];
-            sum[j].x += v.x, sum[j].y += v.y, sum[j].z += v.z, sum[j].w += v.w;
+        for (int i = 0; i < 4; ++i) {
+            const float4 *src = pair + i < end ? source(pair + i) : nullptr;
+            v[i][0] = v[i][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (src) v[i][0] = src[0], v[i][1] = src[kTileM];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[0] += v[i][0].x, f[1] += v[i][0].y, f[2] += v[i][0].z, f[3] += v[i][0].w;
+            f[4] += v[i][1].x, f[5] += v[i][1].y, f[6] += v[i][1].z, f[7] += v[i][1].w;
         }
     }
     const int n = fdiv(t, p.w_tm);
     int m = t - n * p.w_tm.d;
     const int half = p.w_tm.d / 2, g = m >= half;
     m -= g * half;
-    const int r = m * kTileM + row;
-    if (r >= p.F) return;
-    E *out = static_cast<E *>(p.dw[g]) + (size_t)r * p.D;
-#pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-        const int col = n * p.n_cols + 4 * (c + j);
-        const float f[8] = {sum[j].x, sum[j].y, sum[j].z, sum[j].w, sum[j + 1].x, sum[j + 1].y, sum[j + 1].z, sum[j + 1].w};
-        if (col < p.D) st_vec<E, 8>(out + col, f);  // (D is a multiple of 8)
-    }
+    const int r = m * kTileM + row, col = n * p.n_cols + 4 * c;
+    if (r < p.F && col < p.D) st_vec<E, 8>(static_cast<E *>(p.dw[g]) + (size_t)r * p.D + col, f);  // (D: a multiple of 8)
 }
 
-// A row-major matrix [rows][cols] of 16-bit elements at `stride` elements a row, in boxes of 64 columns
-// (128 swizzled bytes) x box_rows.
-bool ffn_map(CUtensorMap *m, const void *base, int dtype, long long rows, long long cols, long long stride, int box_rows) {
+// A row-major matrix [rows][cols] of 16-bit elements at `stride` elements a row, in boxes of 64 (or 32) columns,
+// 128 (64) swizzled bytes, x box_rows.
+bool ffn_map(CUtensorMap *m, const void *base, int dtype, long long rows, long long cols, long long stride, int box_rows,
+             int box_cols = 64) {
     auto enc = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(tensor_map_encoder());
     if (!enc) return false;
     cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
     cuuint64_t strides[1] = {static_cast<cuuint64_t>(stride) * 2};
-    cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
+    cuuint32_t box[2] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
     return enc(m, dtype == 1 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
                const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -731,7 +736,7 @@ template <typename E> cudaError_t grad_launch(const GradParams &p, const GradPla
         if (e != cudaSuccess) return e;
         set_on_devices.fetch_or(bit);
     }
-    ffn_grad_kernel<E><<<2 * g.pairs, kFfnThreads, kGradSmem, stream>>>(p);
+    ffn_grad_kernel<E><<<2 * g.pairs, kGradThreads, kGradSmem, stream>>>(p);
     if ((e = cudaGetLastError()) != cudaSuccess || !g.cut) return e;
     GradSumParams q;
     q.partial = p.partial;
@@ -739,7 +744,7 @@ template <typename E> cudaError_t grad_launch(const GradParams &p, const GradPla
     q.w_tm = p.w_tm;
     q.nk = g.w_nk, q.pairs = g.pairs, q.n_cols = g.n_cols, q.D = p.D, q.F = p.F;
     std::memcpy(q.w_start, g.w_start, sizeof(q.w_start));
-    ffn_grad_sum_kernel<E><<<dim3(g.n_cols / 32, g.w_tiles), kTileM, 0, stream>>>(q);
+    ffn_grad_sum_kernel<E><<<dim3(g.n_cols / 8, g.w_tiles), kTileM, 0, stream>>>(q);
     return cudaGetLastError();
 }
 
@@ -769,7 +774,7 @@ cudaError_t launch_ffn(const FfnProblem &q, void *out, cudaStream_t stream) {
     const cudaError_t e = sm_count(&n_sm);
     if (e != cudaSuccess) return e;
     FfnParams p;
-    if (!ffn_params(q, p) || !ffn_map(&p.o[0], out, q.dtype, q.M, q.F, q.F, 32)) return cudaErrorInvalidValue;
+    if (!ffn_params(q, p) || !ffn_map(&p.o[0], out, q.dtype, q.M, q.F, q.F, 32, 32)) return cudaErrorInvalidValue;
     return ffn_launch<kFwd>(p, q.dtype, n_sm, stream);
 }
 
@@ -788,8 +793,8 @@ cudaError_t launch_ffn_bwd(const FfnProblem &q, const void *dout, long long dout
     if (e != cudaSuccess) return e;
     char *dg = static_cast<char *>(workspace), *dv = dg + act_bytes(q.M, q.F);
     FfnParams p;
-    if (!ffn_params(q, p) || !ffn_map(&p.o[0], dg, q.dtype, q.M, q.F, q.F, 32) ||
-        !ffn_map(&p.o[1], dv, q.dtype, q.M, q.F, q.F, 32) || !ffn_map(&p.dh, dout, q.dtype, q.M, q.F, dout_stride, 32))
+    if (!ffn_params(q, p) || !ffn_map(&p.o[0], dg, q.dtype, q.M, q.F, q.F, 32, 32) ||
+        !ffn_map(&p.o[1], dv, q.dtype, q.M, q.F, q.F, 32, 32) || !ffn_map(&p.dh, dout, q.dtype, q.M, q.F, dout_stride, 32, 32))
         return cudaErrorInvalidValue;
     GradPlan g;
     if (!ffn_grad_plan(q.M, q.D, q.F, n_sm, &g)) return cudaErrorInvalidValue;
@@ -808,7 +813,7 @@ cudaError_t launch_ffn_bwd(const FfnProblem &q, const void *dout, long long dout
     r.w_nk = make_fastdiv(g.w_nk);
     r.x_tiles = g.x_tiles, r.x_nk = g.x_nk, r.x_half = g.x_nk / 2;
     r.n_cols = g.n_cols;
-    const int fit = (kGradSmem - 1024 - 8 * kBox) / (kStageA + 8192 * (g.n_cols / 128));
+    const int fit = (kGradSmem - 1024 - 8 * kGradBox) / (kStageA + 8192 * (g.n_cols / 128));
     r.stages = fit < 8 ? fit : 8;
     r.M = static_cast<int>(q.M), r.D = q.D, r.F = q.F;
     const uint32_t fmt = q.dtype == 1 ? kFmtF16 : kFmtBF16;
