@@ -51,10 +51,15 @@ constexpr int kBox = 32 * 64;      // an epilogue warp's box: 32 rows x 32 colum
 constexpr int kGradBox = 32 * 128; // ... x 64 columns
 constexpr uint64_t kFfnWaitNs = 1000000000ull;
 
-constexpr int ffn_stages(int mode) { return mode == kAct ? 5 : 6; }
+constexpr int kResident = 6;       // blocks of D up to which a tile's weights stay in shared memory
+// Stages: A and B, or with resident weights A alone.
+constexpr int ffn_stages(int mode, bool res) { return mode == kAct ? (res ? 4 : 5) : 6; }
 constexpr int ffn_boxes(int mode) { return mode == kAct ? 2 : 1; }  // staging boxes of a warp: H, or dG, and dH, then dV
-constexpr size_t ffn_smem(int mode) {
-    return (size_t)ffn_stages(mode) * kStageBytes + 16 * (size_t)ffn_boxes(mode) * kBox + 1024;
+constexpr int ffn_box_at(int mode, bool res) {
+    return res ? (kResident + ffn_stages(mode, true)) * kStageA : ffn_stages(mode, false) * kStageBytes;
+}
+constexpr size_t ffn_smem(int mode, bool res) {
+    return (size_t)ffn_box_at(mode, res) + 16 * (size_t)ffn_boxes(mode) * kBox + 1024;
 }
 
 struct FfnParams {
@@ -70,6 +75,7 @@ struct FfnParams {
 
 struct FfnBars {
     uint64_t full[6], empty[6], acc_full[2], acc_empty[2], dh[16];
+    uint64_t w_full[kResident], w_empty[kResident];  // resident weights
     uint32_t tmem, abort;
 };
 
@@ -91,21 +97,29 @@ __device__ __forceinline__ uint64_t kmajor_desc(uint32_t saddr) { return smem_de
 // 64 x 64 blocks, 8 KB apart along M or N
 __device__ __forceinline__ uint64_t mnmajor_desc(uint32_t saddr) { return smem_desc(saddr, 8192, 1024, kLayoutSw128); }
 
-template <int MODE, typename E>
+// RES: D has at most kResident blocks.  A pair then takes a stretch of tiles of the same channels, one below the
+// other, whose weights it loads once: a tile reads 96 KB a CTA instead of 192, which is what bounds short sums (at about
+// 50 bytes a cycle and SM they take 3,900 cycles where the MMAs take 3,072).
+template <int MODE, typename E, bool RES>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_constant__ FfnParams p) {
-    constexpr int S = ffn_stages(MODE), BOXES = ffn_boxes(MODE);
+    constexpr int S = ffn_stages(MODE, RES), BOXES = ffn_boxes(MODE);
+    constexpr uint32_t kStage = RES ? kStageA : kStageBytes, kStages0 = RES ? kResident * kStageA : 0;
     extern __shared__ uint8_t ffn_raw[];
     __shared__ FfnBars bars;
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(ffn_raw) + 1023) & ~uintptr_t(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int tile0 = RES ? static_cast<int>((long long)p.tiles * pair / pairs) : pair;
+    const int tile1 = RES ? static_cast<int>((long long)p.tiles * (pair + 1) / pairs) : p.tiles;
+    const int step = RES ? 1 : pairs;
     volatile uint32_t *abort = &bars.abort;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S; ++i) mbar_init(&bars.full[i], 1), mbar_init(&bars.empty[i], 1);
         for (int i = 0; i < 2; ++i) mbar_init(&bars.acc_full[i], 1), mbar_init(&bars.acc_empty[i], 32);
         for (int i = 0; i < 16; ++i) mbar_init(&bars.dh[i], 1);
+        for (int i = 0; i < kResident; ++i) mbar_init(&bars.w_full[i], 1), mbar_init(&bars.w_empty[i], 1);
         bars.abort = 0;
         fence_mbar_init();
     }
@@ -128,51 +142,73 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
 
     if (warp == 0) {
         if (lane == 0) {
-            // ---- loads: this CTA's half of A's rows and of B's columns, counted on the even CTA's barrier
-            constexpr uint32_t bytes = 2u * kStageBytes;
+            // ---- loads: this CTA's half of A's rows and of B's columns, counted on the even CTA's barriers
             uint32_t it = 0;
+            int held = -1, loads = 0;  // channels whose weights are resident, and how often some were loaded
             bool ok = true;
-            for (int tile = pair; ok && tile < p.tiles; tile += pairs) {
+            for (int tile = tile0; ok && tile < tile1; tile += step) {
                 const int n = fdiv(tile, p.tm), m = tile - n * p.tm.d;
                 for (int k = 0; k < p.nk; ++k, ++it) {
                     const uint32_t s = it % S;
+                    if (RES && n != held) {
+                        if (loads > 0 && !mbar_wait(&bars.w_empty[k], (loads - 1) & 1, abort, kFfnWaitNs)) {
+                            give_up();
+                            ok = false;
+                            break;
+                        }
+                        if (rank == 0) mbar_arrive_expect_tx(&bars.w_full[k], 2 * kStageA);
+                        tma_load_2d_pair(smem_u32(smem) + k * kStageA, &p.b[rank], map_to_cta(smem_u32(&bars.w_full[k]), 0),
+                                         k * kBlockK, n * 128);
+                    }
                     if (it >= S && !mbar_wait(&bars.empty[s], ((it / S) - 1) & 1, abort, kFfnWaitNs)) {
                         give_up();
                         ok = false;
                         break;
                     }
                     const uint32_t bar = map_to_cta(smem_u32(&bars.full[s]), 0);
-                    if (rank == 0) mbar_arrive_expect_tx(&bars.full[s], bytes);
-                    const uint32_t sa = smem_u32(smem) + s * kStageBytes, sb = sa + kStageA;
+                    if (rank == 0) mbar_arrive_expect_tx(&bars.full[s], 2 * kStage);
+                    const uint32_t sa = smem_u32(smem) + kStages0 + s * kStage;
                     tma_load_2d_pair(sa, &p.a, bar, k * kBlockK, m * kTileM + rank * 128);
-                    tma_load_2d_pair(sb, &p.b[rank], bar, k * kBlockK, n * 128);
+                    if (!RES) tma_load_2d_pair(sa + kStageA, &p.b[rank], bar, k * kBlockK, n * 128);
                 }
+                if (n != held) held = n, ++loads;
             }
             // every block consumed: no copy and no barrier arrival is in flight any more
             const uint32_t last = it < S ? it : S;
             for (uint32_t i = it - last; i != it; ++i)
                 if (!mbar_wait(&bars.empty[i % S], (i / S) & 1, nullptr, kFfnWaitNs)) give_up();
+            if (RES && loads > 0) {
+                for (int k = 0; k < p.nk; ++k)
+                    if (!mbar_wait(&bars.w_empty[k], (loads - 1) & 1, nullptr, kFfnWaitNs)) give_up();
+            }
         }
     } else if (warp == 1) {
         if (rank == 0) {
             // ---- MMAs of both CTAs' halves
             uint32_t it = 0, acc = 0;
+            int held = -1, loads = 0;
             bool ok = true;
-            for (int tile = pair; ok && tile < p.tiles; tile += pairs, ++acc) {
+            for (int tile = tile0; ok && tile < tile1; tile += step, ++acc) {
+                const int n = fdiv(tile, p.tm);
                 const uint32_t buf = acc & 1;
                 if (acc >= 2) ok = mbar_wait_cluster(&bars.acc_empty[buf], ((acc >> 1) - 1) & 1, abort, kFfnWaitNs);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
+                const bool fresh = RES && n != held, done = RES && (tile + 1 >= tile1 || fdiv(tile + 1, p.tm) != n);
                 for (int k = 0; k < p.nk; ++k, ++it) {
                     const uint32_t s = it % S;
-                    ok = __all_sync(0xffffffffu, mbar_wait_cluster(&bars.full[s], (it / S) & 1, abort, kFfnWaitNs));
+                    if (fresh) ok = mbar_wait_cluster(&bars.w_full[k], loads & 1, abort, kFfnWaitNs);
+                    ok = __all_sync(0xffffffffu, mbar_wait_cluster(&bars.full[s], (it / S) & 1, abort, kFfnWaitNs) && ok);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t sa = smem_u32(smem) + s * kStageBytes, sb = sa + kStageA;
+                    const uint32_t sa = smem_u32(smem) + kStages0 + s * kStage;
+                    const uint32_t sb = RES ? smem_u32(smem) + k * kStageA : sa + kStageA;
                     mma4_f16_ss_pair<2, 2>(tmem + buf * 256, kmajor_desc(sa), kmajor_desc(sb), p.idesc, k > 0);
                     mma_commit_pair(&bars.empty[s]);
+                    if (done) mma_commit_pair(&bars.w_empty[k]);
                 }
+                if (fresh) held = n, ++loads;
                 if (ok) mma_commit_pair(&bars.acc_full[buf]);
             }
             if (!ok && lane == 0) give_up();
@@ -180,22 +216,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
     } else if (warp >= kFfnEpiWarp) {
         // ---- epilogue: rows 32 (warp % 4) .. of this CTA's 128, a quarter of the 128 channels
         const int w = warp - kFfnEpiWarp, sub = warp & 3, quarter = w >> 2;
-        uint8_t *box = smem + S * kStageBytes + (size_t)w * BOXES * kBox;
+        uint8_t *box = smem + ffn_box_at(MODE, RES) + (size_t)w * BOXES * kBox;
         const uint32_t lanes = static_cast<uint32_t>(sub * 32) << 16;
         const uint32_t acc_empty = map_to_cta(smem_u32(&bars.acc_empty[0]), 0);  // the even CTA's, 8 bytes apart
         // dH of the next tile arrives while its accumulator is filled
         auto load_dh = [&](int tile) {
-            if (tile >= p.tiles) return;
+            if (tile >= tile1) return;
             const int n = fdiv(tile, p.tm), m = tile - n * p.tm.d;
             mbar_arrive_expect_tx(&bars.dh[w], kBox);
             tma_load_2d(box + kBox, &p.dh, &bars.dh[w], n * 128 + quarter * 32,
                         m * kTileM + static_cast<int>(rank) * 128 + sub * 32);
         };
         if constexpr (MODE == kAct) {
-            if (lane == 0) load_dh(pair);
+            if (lane == 0) load_dh(tile0);
         }
         uint32_t acc = 0;
-        for (int tile = pair; tile < p.tiles; tile += pairs, ++acc) {
+        for (int tile = tile0; tile < tile1; tile += step, ++acc) {
             const int n = fdiv(tile, p.tm), m = tile - n * p.tm.d;
             const uint32_t buf = acc & 1;
             const int row0 = m * kTileM + static_cast<int>(rank) * 128 + sub * 32, col0 = n * 128 + quarter * 32;
@@ -257,13 +293,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
                 }
                 if constexpr (MODE == kAct) {
                     bulk_wait_read();  // both boxes have been stored: the next dH may come
-                    load_dh(tile + pairs);
+                    load_dh(tile + step);
                 }
             }
             __syncwarp();
         }
         if constexpr (MODE == kAct) {  // after giving up: the last dH box may still be on its way
-            if (lane == 0 && pair + static_cast<int>(acc) * pairs < p.tiles) mbar_wait(&bars.dh[w], acc & 1, nullptr, kFfnWaitNs);
+            if (lane == 0 && tile0 + static_cast<int>(acc) * step < tile1) mbar_wait(&bars.dh[w], acc & 1, nullptr, kFfnWaitNs);
         }
         if (lane == 0) bulk_wait_all();
     }
@@ -597,25 +633,28 @@ bool ffn_map(CUtensorMap *m, const void *base, int dtype, long long rows, long l
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int MODE, typename E> cudaError_t ffn_launch_typed(const FfnParams &p, int n_sm, cudaStream_t stream) {
+template <int MODE, typename E, bool RES> cudaError_t ffn_launch_typed(const FfnParams &p, int n_sm, cudaStream_t stream) {
     static std::atomic<unsigned long long> set_on_devices(0);
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     const unsigned long long bit = 1ull << (dev & 63);
     if (!(set_on_devices.load(std::memory_order_relaxed) & bit)) {
-        e = cudaFuncSetAttribute(ffn_kernel<MODE, E>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 static_cast<int>(ffn_smem(MODE)));
+        e = cudaFuncSetAttribute(ffn_kernel<MODE, E, RES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 static_cast<int>(ffn_smem(MODE, RES)));
         if (e != cudaSuccess) return e;
         set_on_devices.fetch_or(bit);
     }
     const int pairs = p.tiles < n_sm / 2 ? p.tiles : n_sm / 2;
-    ffn_kernel<MODE, E><<<2 * pairs, kFfnThreads, ffn_smem(MODE), stream>>>(p);
+    ffn_kernel<MODE, E, RES><<<2 * pairs, kFfnThreads, ffn_smem(MODE, RES), stream>>>(p);
     return cudaGetLastError();
 }
 template <int MODE> cudaError_t ffn_launch(const FfnParams &p, int dtype, int n_sm, cudaStream_t stream) {
-    return dtype == 1 ? ffn_launch_typed<MODE, __half>(p, n_sm, stream)
-                      : ffn_launch_typed<MODE, __nv_bfloat16>(p, n_sm, stream);
+    if (p.nk <= kResident)
+        return dtype == 1 ? ffn_launch_typed<MODE, __half, true>(p, n_sm, stream)
+                          : ffn_launch_typed<MODE, __nv_bfloat16, true>(p, n_sm, stream);
+    return dtype == 1 ? ffn_launch_typed<MODE, __half, false>(p, n_sm, stream)
+                      : ffn_launch_typed<MODE, __nv_bfloat16, false>(p, n_sm, stream);
 }
 
 int ceil_div(long long a, int b) { return static_cast<int>((a + b - 1) / b); }
