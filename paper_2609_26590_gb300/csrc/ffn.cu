@@ -321,13 +321,16 @@ struct GradParams {
     CUtensorMap ax[2], bx[2];  // dX: dG, dV by tokens; Wg, Wv by F
     CUtensorMap aw[2], bw;     // dW: dG, dV and the tokens, by tokens (MN-major)
     CUtensorMap o[3];          // dX, dWg, dWv
-    FastDiv x_tm, w_tm, w_nk;  // tiles down dX's rows and down both dW's; 64-deep blocks of a dW tile
+    FastDiv x_tm, w_tm;        // tiles down dX's rows and down both dW's
+    FastDiv x_nk_div, w_nk;    // 64-deep blocks of a tile
     int x_tiles, x_nk, x_half; // dX's tiles, blocks of one, blocks of its first product
     int n_cols, stages;        // accumulator columns: a multiple of 128 up to 512
     int M, D, F;
     uint32_t x_idesc[2], w_idesc[2];  // of the first 256 columns and of the rest
-    float *partial;                   // [2 pairs] tiles of cut sums, [n_cols / 4][256][4] each
+    float *partial;                   // [4 pairs] tiles of cut sums, [n_cols / 4][256][4] each: dW's, then dX's
+    int x_cut;                        // dX's sums are cut too
     int w_start[kGradMaxPairs + 1];   // a pair's blocks of dW: its share of w_tiles x w_nk
+    int x_start[kGradMaxPairs + 1];   // the same of dX where that is cut
 };
 
 struct GradBars {
@@ -342,30 +345,41 @@ struct GradItem {
     int k0, k1;
     int slot;    // of a cut sum, else -1
 };
-// A pair's items in order: its dX tiles, then its stretch of dW.  Every role walks them alike.
+// A pair's items in order: its dX tiles (or stretch of dX), then its stretch of dW.  Every role walks them alike.
 struct GradWalk {
-    int tile, pos, end, pair;
+    int tile, x_pos, x_end, pos, end, pair;
     __device__ __forceinline__ GradWalk(const GradParams &p, int pair_)
-        : tile(pair_), pos(p.w_start[pair_]), end(p.w_start[pair_ + 1]), pair(pair_) {}
+        : tile(pair_), x_pos(p.x_start[pair_]), x_end(p.x_start[pair_ + 1]), pos(p.w_start[pair_]),
+          end(p.w_start[pair_ + 1]), pair(pair_) {}
+    // The next stretch of one tile out of [at, to) of tiles of nk blocks; returns the tile.
+    __device__ __forceinline__ int stretch(GradItem *it, int &at, int to, const FastDiv &nk, int slot0) {
+        const int t = fdiv(at, nk);
+        it->k0 = at - t * nk.d;
+        it->k1 = to - at < nk.d - it->k0 ? it->k0 + to - at : nk.d;
+        at += it->k1 - it->k0;
+        it->slot = it->k1 - it->k0 < nk.d ? slot0 + 2 * pair + (it->k0 == 0) : -1;
+        return t;
+    }
     __device__ __forceinline__ bool next(const GradParams &p, int pairs, GradItem *it) {
         it->g = 0;
-        it->slot = -1;
-        if (tile < p.x_tiles) {
+        if (p.x_cut ? x_pos < x_end : tile < p.x_tiles) {
             it->w = false;
-            it->n = fdiv(tile, p.x_tm);
-            it->m = tile - it->n * p.x_tm.d;
-            it->k0 = 0;
-            it->k1 = p.x_nk;
-            tile += pairs;
+            int t = tile;
+            if (p.x_cut) {
+                t = stretch(it, x_pos, x_end, p.x_nk_div, 2 * pairs);
+            } else {
+                it->k0 = 0;
+                it->k1 = p.x_nk;
+                it->slot = -1;
+                tile += pairs;
+            }
+            it->n = fdiv(t, p.x_tm);
+            it->m = t - it->n * p.x_tm.d;
             return true;
         }
         if (pos >= end) return false;
         it->w = true;
-        const int t = fdiv(pos, p.w_nk), nk = p.w_nk.d;
-        it->k0 = pos - t * nk;
-        it->k1 = end - pos < nk - it->k0 ? it->k0 + end - pos : nk;
-        pos += it->k1 - it->k0;
-        if (it->k1 - it->k0 < nk) it->slot = 2 * pair + (it->k0 == 0);
+        const int t = stretch(it, pos, end, p.w_nk, 0);
         it->n = fdiv(t, p.w_tm);
         it->m = t - it->n * p.w_tm.d;
         const int half = p.w_tm.d / 2;
@@ -529,6 +543,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGradThreads, 1) ffn
                             if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty + 8 * part);
                         }
                         if (cut != nullptr) {
+                            if (row0 + lane < rows && col0 + c * 32 < p.D)  // (what lies outside is not summed)
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
                                 cut[(size_t)((off + c * 32) / 4 + j) * kTileM] =
@@ -567,35 +582,47 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGradThreads, 1) ffn
     if (warp == 2) tmem_dealloc_pair(tmem, 512);
 }
 
-// Sums of dW tiles that were cut between pairs, in the order of K, rounded once.  A CTA takes eight columns of
-// a tile, a thread one of its 256 rows.
+// Sums of tiles that were cut between pairs, in the order of K, rounded once: dX's tiles, then dW's.  A CTA takes eight
+// columns of a tile, a thread one of its 256 rows.
 struct GradSumParams {
     const float *partial;
-    void *dw[2];
-    FastDiv w_tm;
-    int nk, pairs, n_cols, D, F;
-    int w_start[kGradMaxPairs + 1];
+    void *dx, *dw[2];
+    FastDiv x_tm, w_tm;
+    int x_tiles, x_nk, w_nk, pairs, n_cols, M, D, F;  // x_tiles: 0 where dX is not cut
+    int w_start[kGradMaxPairs + 1], x_start[kGradMaxPairs + 1];
 };
 template <typename E> __global__ void __launch_bounds__(kTileM) ffn_grad_sum_kernel(const __grid_constant__ GradSumParams p) {
-    const int t = blockIdx.y, row = threadIdx.x, c = blockIdx.x * 2;  // c: first group of four columns
-    const int first = t * p.nk, last = first + p.nk;
+    const bool w = static_cast<int>(blockIdx.y) >= p.x_tiles;
+    const int t = w ? blockIdx.y - p.x_tiles : blockIdx.y, row = threadIdx.x, c = blockIdx.x * 2;  // c: groups of four columns
+    const int *start = w ? p.w_start : p.x_start;
+    const int nk = w ? p.w_nk : p.x_nk, first = t * nk, last = first + nk;
     int lo = 0, hi = p.pairs - 1;  // the pair that holds the tile's first block
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
-        if (p.w_start[mid] <= first)
+        if (start[mid] <= first)
             lo = mid;
         else
             hi = mid - 1;
     }
-    if (p.w_start[lo + 1] >= last) return;  // a whole tile: stored by its pair
+    if (start[lo + 1] >= last) return;  // a whole tile: stored by its pair
+    const FastDiv &tm = w ? p.w_tm : p.x_tm;
+    const int n = fdiv(t, tm);
+    int m = t - n * tm.d, g = 0;
+    if (w) {
+        const int half = tm.d / 2;
+        g = m >= half;
+        m -= g * half;
+    }
+    const int r = m * kTileM + row, col = n * p.n_cols + 4 * c;
+    if (r >= (w ? p.F : p.M) || col >= p.D) return;
     float f[8] = {};
     auto source = [&](int pair) {  // a pair's stretch, null when it has none of this tile
-        if (p.w_start[pair + 1] <= p.w_start[pair]) return static_cast<const float4 *>(nullptr);
-        const int slot = 2 * pair + (p.w_start[pair] <= first);
+        if (start[pair + 1] <= start[pair]) return static_cast<const float4 *>(nullptr);
+        const int slot = (w ? 0 : 2 * p.pairs) + 2 * pair + (start[pair] <= first);
         return reinterpret_cast<const float4 *>(p.partial) + ((size_t)slot * (p.n_cols / 4) + c) * kTileM + row;
     };
     int end = lo + 1;
-    while (end < p.pairs && p.w_start[end] < last) ++end;
+    while (end < p.pairs && start[end] < last) ++end;
     for (int pair = lo; pair < end; pair += 4) {  // four stretches' loads together, added in order
         float4 v[4][2];
 #pragma unroll
@@ -610,12 +637,7 @@ template <typename E> __global__ void __launch_bounds__(kTileM) ffn_grad_sum_ker
             f[4] += v[i][1].x, f[5] += v[i][1].y, f[6] += v[i][1].z, f[7] += v[i][1].w;
         }
     }
-    const int n = fdiv(t, p.w_tm);
-    int m = t - n * p.w_tm.d;
-    const int half = p.w_tm.d / 2, g = m >= half;
-    m -= g * half;
-    const int r = m * kTileM + row, col = n * p.n_cols + 4 * c;
-    if (r < p.F && col < p.D) st_vec<E, 8>(static_cast<E *>(p.dw[g]) + (size_t)r * p.D + col, f);  // (D: a multiple of 8)
+    st_vec<E, 8>(static_cast<E *>(w ? p.dw[g] : p.dx) + (size_t)r * p.D + col, f);  // (D: a multiple of 8)
 }
 
 // A row-major matrix [rows][cols] of 16-bit elements at `stride` elements a row, in boxes of 64 (or 32) columns,
@@ -671,17 +693,26 @@ bool set_tiles(FfnParams &p, int tm, int tn) {
 struct GradPlan {
     int pairs, n_cols;
     int x_tm, x_tiles, x_nk, w_tm, w_tiles, w_nk;
-    bool cut;                        // some dW tile's sum is cut between pairs
-    int w_start[kGradMaxPairs + 1];
+    bool cut, x_cut;                 // some dW tile's (dX tile's) sum is cut between pairs
+    int w_start[kGradMaxPairs + 1], x_start[kGradMaxPairs + 1];
 };
 
-// Whole tiles (dX's dealt round, then each dW tile to the pair that is least loaded), or dW's blocks of K cut so that
-// all pairs end together, whichever costs less; for each tile width.  A block of K takes a pair the longer of its MMAs
-// (two cycles a column) and of its operands' way into shared memory (50 bytes a cycle and SM was measured, which is what
-// bounds 256 x 256 tiles at about 85 % of the tensor cores' rate; wider ones read A less often), a tile's epilogue
-// about 4,000 cycles, and a cut sum's partial tiles their way to memory and back.
+// A cut at block e of tiles of nk blocks that would leave less than kGradMinCut moves to the tile's end.
+long long snap_cut(long long e, int nk) {
+    const int k = static_cast<int>(e % nk);
+    if (k < kGradMinCut) return e - k;
+    return nk - k < kGradMinCut ? e + (nk - k) : e;
+}
+
+// The cheapest of three ways, each for tiles of 128 to 512 columns: whole tiles (dX's dealt round, then each dW tile to
+// the pair that is least loaded); dX's whole and dW's blocks of K cut so that all pairs end together; or all blocks,
+// dX's and then dW's, in even stretches (few tokens: dX has few tiles and long sums).  A block of K takes a pair the
+// longer of its MMAs (two cycles a column) and of its operands' way into shared memory (50 bytes a cycle and SM was
+// measured, which is what bounds 256 x 256 tiles at about 85 % of the tensor cores' rate; wider ones read A less
+// often), a tile's epilogue about 4,000 cycles, and a cut sum's partial tiles their way to memory and back.
 bool ffn_grad_plan(long long M, int D, int F, int n_sm, GradPlan *out) {
     GradPlan g;
+    std::memset(&g, 0, sizeof(g));
     g.pairs = n_sm / 2 < kGradMaxPairs ? n_sm / 2 : kGradMaxPairs;
     if (g.pairs < 1) return false;
     g.x_nk = 2 * ceil_div(F, kBlockK);
@@ -692,7 +723,7 @@ bool ffn_grad_plan(long long M, int D, int F, int n_sm, GradPlan *out) {
         if (n > 128 && n >= D + 128) break;
         const int tn = ceil_div(D, n);
         const long long xt = (long long)ceil_div(M, kTileM) * tn, wt = 2LL * ceil_div(F, kTileM) * tn;
-        if (xt > (1 << 29) || wt > (1 << 29) || wt * g.w_nk > (1LL << 30)) continue;
+        if (xt * g.x_nk > (1LL << 30) || wt * g.w_nk > (1LL << 30)) continue;
         g.n_cols = n;
         g.x_tm = ceil_div(M, kTileM), g.x_tiles = static_cast<int>(xt);
         g.w_tm = 2 * ceil_div(F, kTileM), g.w_tiles = static_cast<int>(wt);
@@ -719,51 +750,64 @@ bool ffn_grad_plan(long long M, int D, int F, int n_sm, GradPlan *out) {
         if (!found || whole < least) {
             found = true;
             least = whole;
-            g.cut = false;
-            g.w_start[0] = 0;
+            g.cut = g.x_cut = false;
             for (int i = 0; i < g.pairs; ++i) {
                 const int at = i < r ? 0 : 1, rank = i < r ? i : i - r;
                 g.w_start[i + 1] = g.w_start[i] + (count[at] + (rank < extra[at])) * g.w_nk;
             }
             *out = g;
         }
-        // cut sums: an even share of the blocks for every pair, after its dX tiles
-        const long long blocks = (long long)g.w_tiles * g.w_nk;
-        double share = (blocks * block + g.x_tiles * x_cost) / g.pairs;  // all pairs' end, if none has too much already
-        if (share < (q + 1) * x_cost && r > 0 && r < g.pairs)
-            share = q * x_cost + blocks * block / (g.pairs - r);  // the pairs with one dX tile more take none
-        const double tiles = std::min(g.pairs + g.w_tiles, 2 * g.pairs);
         // partial tiles written and read at about 20 bytes a cycle and SM, the sum's launch and tail
-        const double cost = std::max(share, r > 0 ? own[0] : 0.0) + 2 * tiles * kTileM * n * 4.0 / (20.0 * n_sm) + 16000;
-        if (cost < least && g.w_nk >= 4 * kGradMinCut && g.w_tiles <= 65535) {
+        auto partial = [&](int tiles, long long rows) {
+            return 2.0 * std::min(g.pairs + tiles, 2 * g.pairs) * std::min<long long>(rows, kTileM) * n * 4.0 / (20.0 * n_sm);
+        };
+        const long long w_blocks = (long long)g.w_tiles * g.w_nk, x_blocks = (long long)g.x_tiles * g.x_nk;
+        if (g.x_tiles + g.w_tiles > 65535) continue;  // (the sum's grid)
+        // dW cut: an even share of the blocks for every pair, after its dX tiles
+        double share = (w_blocks * block + g.x_tiles * x_cost) / g.pairs;  // all pairs' end, if none has too much already
+        if (r > 0 && share < own[0]) share = own[1] + w_blocks * block / (g.pairs - r);  // the first r pairs take none
+        const double cost = std::max(share, r > 0 ? own[0] : 0.0) + partial(g.w_tiles, F) + 16000;
+        if (cost < least && g.w_nk >= 4 * kGradMinCut) {
             least = cost;
-            g.cut = true;
+            g.cut = true, g.x_cut = false;
             double at = 0;
-            g.w_start[0] = 0;
             for (int i = 0; i < g.pairs; ++i) {
                 const double left = share - (q + (i < r)) * x_cost;
                 if (left > 0) at += left / block;
-                long long e = static_cast<long long>(at + 0.5);
-                const int k = static_cast<int>(e % g.w_nk);  // no stretch shorter than kGradMinCut at a tile's ends
-                if (k < kGradMinCut)
-                    e -= k;
-                else if (g.w_nk - k < kGradMinCut)
-                    e += g.w_nk - k;
-                if (e > blocks || i + 1 == g.pairs) e = blocks;
-                if (e < g.w_start[i]) e = g.w_start[i];
-                g.w_start[i + 1] = static_cast<int>(e);
+                long long e = snap_cut(static_cast<long long>(at + 0.5), g.w_nk);
+                if (e > w_blocks || i + 1 == g.pairs) e = w_blocks;
+                g.w_start[i + 1] = std::max(static_cast<int>(e), g.w_start[i]);
             }
             *out = g;
+        }
+        // both cut: even stretches of all blocks, a tile's epilogue counting as `tail` blocks behind its own
+        const int tail = static_cast<int>(4000 / block + 0.5), xv = g.x_nk + tail, wv = g.w_nk + tail;
+        const long long x_all = (long long)g.x_tiles * xv, all = x_all + (long long)g.w_tiles * wv;
+        const long long piece = std::max<long long>((all + g.pairs - 1) / g.pairs, kGradMinCut);
+        const double both = piece * block + partial(g.x_tiles, M) + (g.w_nk >= 2 * kGradMinCut ? partial(g.w_tiles, F) : 0) + 16000;
+        if (both < least) {
+            least = both;
+            g.cut = g.x_cut = true;
+            auto block_at = [](long long v, int virt, int nk) { return v / virt * nk + std::min<long long>(v % virt, nk); };
+            for (int i = 0; i < g.pairs; ++i) {
+                const long long to = i + 1 == g.pairs ? all : std::min((i + 1) * piece, all);
+                const long long ex = to < x_all ? snap_cut(block_at(to, xv, g.x_nk), g.x_nk) : x_blocks;
+                const long long ew = to == all ? w_blocks : to > x_all ? snap_cut(block_at(to - x_all, wv, g.w_nk), g.w_nk) : 0;
+                g.x_start[i + 1] = std::max(static_cast<int>(ex), g.x_start[i]);
+                g.w_start[i + 1] = std::max(static_cast<int>(ew), g.w_start[i]);
+            }
+            *out = g;
+            std::memset(g.x_start, 0, sizeof(g.x_start));
         }
     }
     return found;
 }
 size_t grad_partial_bytes(const GradPlan &g) {
-    return g.cut ? (size_t)2 * g.pairs * kTileM * g.n_cols * sizeof(float) : 0;
+    return g.cut ? (size_t)(g.x_cut ? 4 : 2) * g.pairs * kTileM * g.n_cols * sizeof(float) : 0;
 }
 size_t act_bytes(long long M, int F) { return ((size_t)M * F * 2 + 255) / 256 * 256; }
 
-template <typename E> cudaError_t grad_launch(const GradParams &p, const GradPlan &g, void *dw_gate, void *dw_value,
+template <typename E> cudaError_t grad_launch(const GradParams &p, const GradPlan &g, void *dx, void *dw_gate, void *dw_value,
                                               cudaStream_t stream) {
     static std::atomic<unsigned long long> set_on_devices(0);
     int dev = 0;
@@ -779,11 +823,13 @@ template <typename E> cudaError_t grad_launch(const GradParams &p, const GradPla
     if ((e = cudaGetLastError()) != cudaSuccess || !g.cut) return e;
     GradSumParams q;
     q.partial = p.partial;
-    q.dw[0] = dw_gate, q.dw[1] = dw_value;
-    q.w_tm = p.w_tm;
-    q.nk = g.w_nk, q.pairs = g.pairs, q.n_cols = g.n_cols, q.D = p.D, q.F = p.F;
+    q.dx = dx, q.dw[0] = dw_gate, q.dw[1] = dw_value;
+    q.x_tm = p.x_tm, q.w_tm = p.w_tm;
+    q.x_tiles = g.x_cut ? g.x_tiles : 0;
+    q.x_nk = g.x_nk, q.w_nk = g.w_nk, q.pairs = g.pairs, q.n_cols = g.n_cols, q.M = p.M, q.D = p.D, q.F = p.F;
     std::memcpy(q.w_start, g.w_start, sizeof(q.w_start));
-    ffn_grad_sum_kernel<E><<<dim3(g.n_cols / 8, g.w_tiles), kTileM, 0, stream>>>(q);
+    std::memcpy(q.x_start, g.x_start, sizeof(q.x_start));
+    ffn_grad_sum_kernel<E><<<dim3(g.n_cols / 8, q.x_tiles + g.w_tiles), kTileM, 0, stream>>>(q);
     return cudaGetLastError();
 }
 
@@ -849,7 +895,9 @@ cudaError_t launch_ffn_bwd(const FfnProblem &q, const void *dout, long long dout
         return cudaErrorInvalidValue;
     r.x_tm = make_fastdiv(g.x_tm);
     r.w_tm = make_fastdiv(g.w_tm);
+    r.x_nk_div = make_fastdiv(g.x_nk);
     r.w_nk = make_fastdiv(g.w_nk);
+    r.x_cut = g.x_cut;
     r.x_tiles = g.x_tiles, r.x_nk = g.x_nk, r.x_half = g.x_nk / 2;
     r.n_cols = g.n_cols;
     const int fit = (kGradSmem - 1024 - 8 * kGradBox) / (kStageA + 8192 * (g.n_cols / 128));
@@ -861,8 +909,9 @@ cudaError_t launch_ffn_bwd(const FfnProblem &q, const void *dout, long long dout
     r.w_idesc[0] = instr_desc(fmt, kTileM, n1, 1, 1), r.w_idesc[1] = instr_desc(fmt, kTileM, n2, 1, 1);
     r.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + 2 * act_bytes(q.M, q.F));
     std::memcpy(r.w_start, g.w_start, sizeof(r.w_start));
-    return q.dtype == 1 ? grad_launch<__half>(r, g, dw_gate, dw_value, stream)
-                        : grad_launch<__nv_bfloat16>(r, g, dw_gate, dw_value, stream);
+    std::memcpy(r.x_start, g.x_start, sizeof(r.x_start));
+    return q.dtype == 1 ? grad_launch<__half>(r, g, dx, dw_gate, dw_value, stream)
+                        : grad_launch<__nv_bfloat16>(r, g, dx, dw_gate, dw_value, stream);
 }
 
 cudaError_t read_and_clear_ffn_status(unsigned int *status) {
