@@ -103,23 +103,49 @@ __global__ void __launch_bounds__(kConvThreads, 3) conv_kernel(const __grid_cons
     };
 #pragma unroll
     for (int i = 0; i < (ASYNC ? kConvDepth : 1); ++i) fetch();
-    float w[W][VEC], bias[VEC], win[W][VEC];  // win: inputs s - W + 1 .. s
-    load_taps<VEC, W>(p.w + (long long)c * W, w);
+    // taps, bias and the window of inputs s - W + 1 .. s, as packed pairs (a single channel: the upper half unused)
+    constexpr int P = (VEC + 1) / 2;
+    f2 w[W][P], bias[P], win[W][P];
+    auto pairs = [](const float (&f)[VEC], f2(&g)[P]) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) bias[i] = p.b ? p.b[c + i] : 0.f;
+        for (int i = 0; i < P; ++i) g[i] = pack2(f[2 * i], 2 * i + 1 < VEC ? f[(2 * i + 1) % VEC] : 0.f);
+    };
+    auto widen = [&](const Raw &r, f2(&g)[P]) {
+        float f[VEC];
+        Vec<E, VEC>::unpack(r, f);
+        pairs(f, g);
+    };
+    {
+        float taps[W][VEC], f[VEC];
+        load_taps<VEC, W>(p.w + (long long)c * W, taps);
+#pragma unroll
+        for (int j = 0; j < W; ++j) pairs(taps[j], w[j]);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) f[i] = p.b ? p.b[c + i] : 0.f;
+        pairs(f, bias);
+    }
 #pragma unroll
     for (int j = 1; j < W; ++j) {  // inputs s0 - W + j
         const int s = s0 - W + j;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) win[j][i] = 0.f;
+        for (int i = 0; i < P; ++i) win[j][i] = 0;
         if (s >= 0) {
             ScanPos q;
             q.set(p.grid, s);
-            Vec<E, VEC>::unpack(ld_vec<E, VEC>(x + (long long)q.t * p.x_stride), win[j]);
+            widen(ld_vec<E, VEC>(x + (long long)q.t * p.x_stride), win[j]);
         } else if (init) {
-            Vec<E, VEC>::unpack(ld_vec<E, VEC>(init + (long long)(s + W - 1) * p.E), win[j]);
+            widen(ld_vec<E, VEC>(init + (long long)(s + W - 1) * p.E), win[j]);
         }
     }
+    auto narrow = [](const f2(&g)[P]) {
+        float f[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float2 a = unpack2(g[i / 2]);
+            f[i] = i % 2 ? a.y : a.x;
+        }
+        return Vec<E, VEC>::pack(f);
+    };
     for (int s = s0; s < s1; s += kConvBatch) {
         Raw now[kConvBatch];
         if constexpr (ASYNC) asm volatile("cp.async.wait_group %0;" ::"n"(kConvDepth - 1) : "memory");
@@ -137,17 +163,20 @@ __global__ void __launch_bounds__(kConvThreads, 3) conv_kernel(const __grid_cons
 #pragma unroll
             for (int j = 0; j + 1 < W; ++j)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) win[j][i] = win[j + 1][i];
-            Vec<E, VEC>::unpack(now[k], win[W - 1]);
-            float a[VEC];
+                for (int i = 0; i < P; ++i) win[j][i] = win[j + 1][i];
+            widen(now[k], win[W - 1]);
+            f2 a[P];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
+            for (int i = 0; i < P; ++i) {
                 a[i] = bias[i];
 #pragma unroll
-                for (int j = 0; j < W; ++j) a[i] = fmaf(w[j][i], win[j][i], a[i]);
-                if (p.silu) a[i] = silu<E>(a[i]);
+                for (int j = 0; j < W; ++j) a[i] = fma2(w[j][i], win[j][i], a[i]);
             }
-            st_vec<E, VEC>(out + (long long)pos.t * p.E, a);
+            if (p.silu) {
+#pragma unroll
+                for (int i = 0; i < P; ++i) a[i] = silu_pair<E>(a[i]);
+            }
+            *reinterpret_cast<Raw *>(out + (long long)pos.t * p.E) = narrow(a);
             pos.next(p.grid);
         }
     }
@@ -155,7 +184,7 @@ __global__ void __launch_bounds__(kConvThreads, 3) conv_kernel(const __grid_cons
     if (p.state && s1 == T) {  // the window's last W - 1 inputs (exact: they are stored values)
         E *st = static_cast<E *>(p.state) + (long long)b * (W - 1) * p.E + c;
 #pragma unroll
-        for (int j = 0; j + 1 < W; ++j) st_vec<E, VEC>(st + (long long)j * p.E, win[j + 1]);
+        for (int j = 0; j + 1 < W; ++j) *reinterpret_cast<Raw *>(st + (long long)j * p.E) = narrow(win[j + 1]);
     }
 }
 

@@ -7,6 +7,8 @@
 
 #include <cstdint>
 
+#include "f32x2.cuh"
+
 namespace gtr {
 
 __device__ __forceinline__ float to_f32(float a) { return a; }
@@ -88,11 +90,45 @@ template <typename E, int VEC> __device__ __forceinline__ void st_vec(E *p, cons
     *reinterpret_cast<typename Vec<E, VEC>::raw *>(p) = Vec<E, VEC>::pack(f);
 }
 
+// The same as packed fp32 pairs.
+template <typename E, int VEC> __device__ __forceinline__ void unpack_pairs(const typename Vec<E, VEC>::raw &r, f2 (&f)[VEC / 2]) {
+    float v[VEC];
+    Vec<E, VEC>::unpack(r, v);
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) f[i] = pack2(v[2 * i], v[2 * i + 1]);
+}
+template <typename E, int VEC> __device__ __forceinline__ typename Vec<E, VEC>::raw pack_pairs(const f2 (&f)[VEC / 2]) {
+    float v[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) {
+        const float2 a = unpack2(f[i]);
+        v[2 * i] = a.x, v[2 * i + 1] = a.y;
+    }
+    return Vec<E, VEC>::pack(v);
+}
+
 // SiLU(z) = z / (1 + e^{-z}).  16-bit outputs take the hardware's power and reciprocal (a few
 // 2^-22 of the value); fp32 outputs the library's exponential and an exact division.
 template <typename E> __device__ __forceinline__ float silu(float z) {
     return __fdividef(z, 1.f + __expf(-z));
 }
 template <> __device__ __forceinline__ float silu<float>(float z) { return z / (1.f + expf(-z)); }
+// The same of a pair.  (Flushing subnormal results of the hardware's functions changes nothing: 1 + e is 1 there, and
+// z / (1 + e) is below 2^-120 where 1 / (1 + e) is.)
+template <typename E> __device__ __forceinline__ f2 silu_pair(f2 z) {
+    const float kNegLog2e = -1.4426950408889634f;
+    const float2 t = unpack2(mul2(z, pack2(kNegLog2e, kNegLog2e)));
+    float e0, e1, r0, r1;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(t.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(t.y));
+    const float2 d = unpack2(add2(pack2(e0, e1), pack2(1.f, 1.f)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(d.y));
+    return mul2(z, pack2(r0, r1));
+}
+template <> __device__ __forceinline__ f2 silu_pair<float>(f2 z) {
+    const float2 t = unpack2(z);
+    return pack2(silu<float>(t.x), silu<float>(t.y));
+}
 
 }  // namespace gtr

@@ -14,7 +14,9 @@
 // kernel adds the partial rows in a fixed order (no atomics: the same bits every time).
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "elem.cuh"
 #include "gla_internal.h"
@@ -25,7 +27,9 @@ namespace {
 
 constexpr int kLnThreads = 128;  // CTA of sub-warp and warp teams
 constexpr int kLnElems = 16;     // elements of a row a thread holds at most
-constexpr int kLnBlockElems = 8; // of a row of up to 8,192 that a whole CTA holds (64 registers a thread)
+constexpr int kLnBlockElems = 8; // of a row that a whole CTA holds, as long as the CTA's threads suffice
+// Threads of a CTA team: 64 registers a thread hold 8 elements of the forward pass, the backward pass's take 128.
+constexpr int kLnFwdThreads = 1024, kLnBwdThreads = 512, kLnMostThreads = 1024;
 
 template <int G> __device__ __forceinline__ float lane_sum(float a) {
 #pragma unroll
@@ -75,7 +79,6 @@ template <int G> struct LnPlace {
         }
     }
 };
-constexpr int ln_max_threads(int g) { return g > 0 ? kLnThreads : 1024; }
 
 // A thread's vectors of the rows to come, NT tensors.  Vectors of 4 bytes and more are copied to the thread's own
 // slots of shared memory some rows ahead (nothing but the thread's own wait is between copy and use); single
@@ -87,139 +90,226 @@ template <typename E, int VEC, int K, int G, int NT> struct LnAhead {
     static constexpr int kDepth = !kAsync ? 1 : G > 0 ? 4 : K * VEC * sizeof(E) <= 16 ? 4 : K * VEC * sizeof(E) <= 32 ? (sizeof(E) == 4 ? 3 : 2) : 1;
     static constexpr size_t smem(int threads) { return kAsync ? sizeof(Raw) * kDepth * NT * K * threads : 0; }
     Raw reg[kAsync ? 1 : NT][kAsync ? 1 : K];
-    uint8_t *base;
-    int slot = 0;
+    uint32_t first, slot, pitch;  // the thread's first slot, the slot of the oldest row, bytes between its vectors
 
-    __device__ __forceinline__ Raw *at(int s, int n, int k) {
-        return reinterpret_cast<Raw *>(base) + (static_cast<size_t>((s * NT + n) * K + k) * blockDim.x + threadIdx.x);
+    __device__ __forceinline__ explicit LnAhead(const void *smem) {
+        pitch = static_cast<uint32_t>(sizeof(Raw)) * (G > 0 ? kLnThreads : blockDim.x);
+        first = slot = ptx::smem_u32(smem) + static_cast<uint32_t>(sizeof(Raw)) * threadIdx.x;
     }
-    // The next row's vectors (row: its first element per tensor), or nothing.
-    __device__ __forceinline__ void fetch(const E *const (&row)[NT], bool live, int rank, int width, int D) {
+    // The next row's vectors (src: the thread's first one per tensor, `step` elements apart) that lie in the row.
+    __device__ __forceinline__ void fetch(const E *const (&src)[NT], bool live, uint32_t mask, int step) {
+        // (predicates, not branches: with single elements there are 16 of them)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int c = (k * width + rank) * VEC;
-            if (live && c < D) {
+            const bool in = live && (mask >> k & 1);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if constexpr (!kAsync) {
-                        reg[n][k] = *reinterpret_cast<const Raw *>(row[n] + c);
-                    } else if constexpr (sizeof(Raw) == 16) {
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(at(slot, n, k))),
-                                     "l"(row[n] + c)
-                                     : "memory");
-                    } else {
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(ptx::smem_u32(at(slot, n, k))),
-                                     "l"(row[n] + c), "n"(sizeof(Raw))
-                                     : "memory");
-                    }
+            for (int n = 0; n < NT; ++n) {
+                const E *from = src[n] + k * step;
+                if constexpr (!kAsync) {
+                    if (in) reg[n][k] = *reinterpret_cast<const Raw *>(from);
+                } else if constexpr (sizeof(Raw) == 16) {
+                    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::
+                                     "r"(slot + (n * K + k) * pitch), "l"(from), "r"(static_cast<uint32_t>(in))
+                                 : "memory");
+                } else {
+                    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], %3;\n\t}" ::
+                                     "r"(slot + (n * K + k) * pitch), "l"(from), "r"(static_cast<uint32_t>(in)), "n"(sizeof(Raw))
+                                 : "memory");
                 }
             }
         }
         if constexpr (kAsync) {
             asm volatile("cp.async.commit_group;" ::: "memory");
-            slot = slot + 1 == kDepth ? 0 : slot + 1;
+            slot += NT * K * pitch;
+            if (slot == first + kDepth * NT * K * pitch) slot = first;
         }
     }
-    // Vectors of the oldest row fetched (`fetch` then refills its slot).
+    // Waits for the vectors of the oldest row fetched (`fetch` then refills its slot).
     __device__ __forceinline__ void ready() {
         if constexpr (kAsync) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
     }
     __device__ __forceinline__ Raw get(int n, int k) {
-        if constexpr (kAsync) return *at(slot, n, k);
-        return reg[n][k];
+        if constexpr (!kAsync) {
+            return reg[n][k];
+        } else if constexpr (sizeof(Raw) == 16) {
+            uint32_t w[4];
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                         : "r"(slot + (n * K + k) * pitch)
+                         : "memory");
+            if constexpr (sizeof(E) == 4)
+                return make_float4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]));
+            else
+                return make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            uint32_t w;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(slot + (n * K + k) * pitch) : "memory");
+            if constexpr (sizeof(E) == 4)
+                return __uint_as_float(w);
+            else
+                return w;
+        }
     }
 };
+// Which of a thread's vectors lie in the row.
+template <int VEC, int K> __device__ __forceinline__ uint32_t ln_mask(int rank, int width, int D) {
+    uint32_t mask = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) mask |= static_cast<uint32_t>((k * width + rank) * VEC < D) << k;
+    return mask;
+}
+
+// What a thread computes with: packed pairs of a vector's elements, or the single element.
+template <int VEC> using LnNum = std::conditional_t<VEC == 1, float, f2>;
+template <int VEC> constexpr int kLnNums = VEC == 1 ? 1 : VEC / 2;
+__device__ __forceinline__ float ln_mul(float a, float b) { return a * b; }
+__device__ __forceinline__ float ln_add(float a, float b) { return a + b; }
+__device__ __forceinline__ float ln_fma(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ f2 ln_mul(f2 a, f2 b) { return mul2(a, b); }
+__device__ __forceinline__ f2 ln_add(f2 a, f2 b) { return add2(a, b); }
+__device__ __forceinline__ f2 ln_fma(f2 a, f2 b, f2 c) { return fma2(a, b, c); }
+template <typename T> __device__ __forceinline__ T ln_splat(float a);
+template <> __device__ __forceinline__ float ln_splat<float>(float a) { return a; }
+template <> __device__ __forceinline__ f2 ln_splat<f2>(float a) { return pack2(a, a); }
+__device__ __forceinline__ float ln_join(float a) { return a; }
+__device__ __forceinline__ float ln_join(f2 a) {
+    const float2 v = unpack2(a);
+    return v.x + v.y;
+}
+template <int P> __device__ __forceinline__ float ln_elem(const float (&f)[P], int i) { return f[i]; }
+template <int P> __device__ __forceinline__ float ln_elem(const f2 (&f)[P], int i) {
+    const float2 v = unpack2(f[i / 2]);
+    return i % 2 ? v.y : v.x;
+}
+template <typename E, int VEC>
+__device__ __forceinline__ void ln_widen(const typename Vec<E, VEC>::raw &r, LnNum<VEC> (&f)[kLnNums<VEC>]) {
+    if constexpr (VEC > 1)
+        unpack_pairs<E, VEC>(r, f);
+    else
+        f[0] = to_f32(r);
+}
+template <typename E, int VEC>
+__device__ __forceinline__ typename Vec<E, VEC>::raw ln_narrow(const LnNum<VEC> (&f)[kLnNums<VEC>]) {
+    if constexpr (VEC > 1)
+        return pack_pairs<E, VEC>(f);
+    else
+        return from_f32<E>(f[0]);
+}
+// Elements c .. c + VEC - 1 of a parameter vector (null: `without`).
+template <int VEC>
+__device__ __forceinline__ void ln_params(const float *v, int c, int D, float without, LnNum<VEC> (&f)[kLnNums<VEC>]) {
+    float t[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) t[i] = v && c + i < D ? v[c + i] : without;
+    if constexpr (VEC > 1) {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) f[i] = pack2(t[2 * i], t[2 * i + 1]);
+    } else {
+        f[0] = t[0];
+    }
+}
 
 // Columns of thread-vector k: (k width + rank) VEC.
-template <typename E, int VEC, int K, int G>
-__global__ void __launch_bounds__(ln_max_threads(G), 1) ln_fwd_kernel(const __grid_constant__ LnParams p) {
+template <typename E, int VEC, int K, int G, int MAXT>
+__global__ void __launch_bounds__(MAXT, 1) ln_fwd_kernel(const __grid_constant__ LnParams p) {
     using Ahead = LnAhead<E, VEC, K, G, 1>;
     extern __shared__ float4 ln_smem[];
     __shared__ float buf[2][1][32];
     const LnPlace<G> at;
     const float inv = 1.f / static_cast<float>(p.D);
     const long long step = (long long)gridDim.x * at.kTeams;
-    Ahead ahead;
-    ahead.base = reinterpret_cast<uint8_t *>(ln_smem);
+    Ahead ahead(ln_smem);
+    const uint32_t mask = ln_mask<VEC, K>(at.rank, at.width, p.D);
     long long next = (long long)blockIdx.x * at.kTeams + at.team;
+    const E *src[1] = {static_cast<const E *>(p.x) + next * p.x_stride + at.rank * VEC};
     auto fetch = [&] {
-        const E *row[1] = {static_cast<const E *>(p.x) + next * p.x_stride};
-        ahead.fetch(row, next < p.rows, at.rank, at.width, p.D);
+        ahead.fetch(src, next < p.rows, mask, at.width * VEC);
         next += step;
+        src[0] += step * p.x_stride;
     };
 #pragma unroll
     for (int i = 0; i < Ahead::kDepth; ++i) fetch();
-    float w[K][VEC], b[K][VEC];
+    using T = LnNum<VEC>;
+    constexpr int P = kLnNums<VEC>;
+    T w[K][P], b[K][P];
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const int c = (k * at.width + at.rank) * VEC + i;
-            w[k][i] = p.w && c < p.D ? p.w[c] : 1.f;
-            b[k][i] = p.b && c < p.D ? p.b[c] : 0.f;
-        }
+    for (int k = 0; k < K; ++k) {
+        const int c = (k * at.width + at.rank) * VEC;
+        ln_params<VEC>(p.w, c, p.D, 1.f, w[k]);
+        ln_params<VEC>(p.b, c, p.D, 0.f, b[k]);
+    }
     // whole warps stay in the loop together (their shuffles name all lanes)
     for (long long base = (long long)blockIdx.x * at.kTeams; base < p.rows; base += step) {
         const long long row = base + at.team;
         const bool live = row < p.rows;
-        float v[K][VEC], s[1] = {0.f};
+        T v[K][P], sum = 0;
         ahead.ready();
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (live && (k * at.width + at.rank) * VEC < p.D) {
-                Vec<E, VEC>::unpack(ahead.get(0, k), v[k]);
+            const bool in = live && (mask >> k & 1);
+            if (VEC == 1 || in) {  // (a slot that no copy wrote holds anything: it counts as zero)
+                ln_widen<E, VEC>(ahead.get(0, k), v[k]);
+                if (VEC == 1 && !in) v[k][0] = 0;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) s[0] += v[k][i];
+                for (int i = 0; i < P; ++i) sum = ln_add(sum, v[k][i]);
             }
         }
         fetch();
+        float s[1] = {ln_join(sum)};
         team_sum<G>(s, buf[0]);
         const float m = s[0] * inv;
-        s[0] = 0.f;
+        sum = 0;
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (live && (k * at.width + at.rank) * VEC < p.D) {
+        for (int k = 0; k < K; ++k) {
+            const bool in = live && (mask >> k & 1);
+            if (VEC == 1 || in) {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    v[k][i] -= m;
-                    s[0] = fmaf(v[k][i], v[k][i], s[0]);
+                for (int i = 0; i < P; ++i) {
+                    v[k][i] = ln_add(v[k][i], ln_splat<T>(-m));
+                    if (VEC == 1 && !in) v[k][i] = 0;
+                    sum = ln_fma(v[k][i], v[k][i], sum);
                 }
             }
+        }
+        s[0] = ln_join(sum);
         team_sum<G>(s, buf[1]);
         const float r = rsqrtf(fmaf(s[0], inv, p.eps));
         if (live && at.rank == 0) {
             if (p.mean) p.mean[row] = m;
             if (p.rstd) p.rstd[row] = r;
         }
-        E *y = static_cast<E *>(p.out) + row * p.D;
+        E *y = static_cast<E *>(p.out) + row * p.D + at.rank * VEC;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int c = (k * at.width + at.rank) * VEC;
-            if (live && c < p.D) {
+            const int c = k * at.width * VEC;
+            if (live && (mask >> k & 1)) {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) v[k][i] = fmaf(v[k][i] * r, w[k][i], b[k][i]);
-                st_vec<E, VEC>(y + c, v[k]);
+                for (int i = 0; i < P; ++i) v[k][i] = ln_fma(ln_mul(v[k][i], ln_splat<T>(r)), w[k][i], b[k][i]);
+                *reinterpret_cast<typename Vec<E, VEC>::raw *>(y + c) = ln_narrow<E, VEC>(v[k]);
             }
         }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-template <typename E, int VEC, int K, int G>
-__global__ void __launch_bounds__(ln_max_threads(G), G > 0 ? 4 : 1) ln_bwd_kernel(const __grid_constant__ LnParams p) {
+template <typename E, int VEC, int K, int G, int MAXT>
+__global__ void __launch_bounds__(MAXT, G > 0 ? 4 : 1) ln_bwd_kernel(const __grid_constant__ LnParams p) {
     using Ahead = LnAhead<E, VEC, K, G, 2>;
     extern __shared__ float4 ln_smem[];
     __shared__ float buf[2][2][32];
     const LnPlace<G> at;
     const float inv = 1.f / static_cast<float>(p.D);
     const long long step = (long long)gridDim.x * at.kTeams;
-    Ahead ahead;
-    ahead.base = reinterpret_cast<uint8_t *>(ln_smem);
+    Ahead ahead(ln_smem);
+    const uint32_t mask = ln_mask<VEC, K>(at.rank, at.width, p.D);
     long long next = (long long)blockIdx.x * at.kTeams + at.team;
+    const E *src[2] = {static_cast<const E *>(p.x) + next * p.x_stride + at.rank * VEC,
+                       static_cast<const E *>(p.dy) + next * p.dy_stride + at.rank * VEC};
     auto fetch = [&] {
-        const E *row[2] = {static_cast<const E *>(p.x) + next * p.x_stride, static_cast<const E *>(p.dy) + next * p.dy_stride};
-        ahead.fetch(row, next < p.rows, at.rank, at.width, p.D);
+        ahead.fetch(src, next < p.rows, mask, at.width * VEC);
         next += step;
+        src[0] += step * p.x_stride;
+        src[1] += step * p.dy_stride;
     };
 #pragma unroll
     for (int i = 0; i < Ahead::kDepth; ++i) fetch();
@@ -228,49 +318,51 @@ __global__ void __launch_bounds__(ln_max_threads(G), G > 0 ? 4 : 1) ln_bwd_kerne
         if (row < p.rows) next_m = p.mean[row], next_r = p.rstd[row];
     };
     stats((long long)blockIdx.x * at.kTeams + at.team);
-    float w[K][VEC], dw[K][VEC] = {}, db[K][VEC] = {};
+    using T = LnNum<VEC>;
+    constexpr int P = kLnNums<VEC>;
+    T w[K][P], dw[K][P] = {}, db[K][P] = {};
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const int c = (k * at.width + at.rank) * VEC + i;
-            w[k][i] = p.w && c < p.D ? p.w[c] : 1.f;
-        }
+    for (int k = 0; k < K; ++k) ln_params<VEC>(p.w, (k * at.width + at.rank) * VEC, p.D, 1.f, w[k]);
     int flip = 0;
     for (long long base = (long long)blockIdx.x * at.kTeams; base < p.rows; base += step, flip ^= 1) {
         const long long row = base + at.team;
         const bool live = row < p.rows;
         const float m = next_m, r = next_r;
         stats(row + step);
-        float h[K][VEC], d[K][VEC], s[2] = {0.f, 0.f};
+        T h[K][P], d[K][P], s0 = 0, s1 = 0;
+        const T minus_m = ln_splat<T>(-m), r2 = ln_splat<T>(r);
         ahead.ready();
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (live && (k * at.width + at.rank) * VEC < p.D) {
-                Vec<E, VEC>::unpack(ahead.get(0, k), h[k]);
-                Vec<E, VEC>::unpack(ahead.get(1, k), d[k]);
+            const bool in = live && (mask >> k & 1);
+            if (VEC == 1 || in) {  // (a slot that no copy wrote holds anything: xh and dy count as zero)
+                ln_widen<E, VEC>(ahead.get(0, k), h[k]);
+                ln_widen<E, VEC>(ahead.get(1, k), d[k]);
+                if (VEC == 1 && !in) h[k][0] = ln_splat<T>(m), d[k][0] = 0;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    h[k][i] = (h[k][i] - m) * r;
-                    dw[k][i] = fmaf(d[k][i], h[k][i], dw[k][i]);
-                    db[k][i] += d[k][i];
-                    d[k][i] *= w[k][i];
-                    s[0] += d[k][i];
-                    s[1] = fmaf(d[k][i], h[k][i], s[1]);
+                for (int i = 0; i < P; ++i) {
+                    h[k][i] = ln_mul(ln_add(h[k][i], minus_m), r2);
+                    dw[k][i] = ln_fma(d[k][i], h[k][i], dw[k][i]);
+                    db[k][i] = ln_add(db[k][i], d[k][i]);
+                    d[k][i] = ln_mul(d[k][i], w[k][i]);
+                    s0 = ln_add(s0, d[k][i]);
+                    s1 = ln_fma(d[k][i], h[k][i], s1);
                 }
             }
         }
         fetch();
+        float s[2] = {ln_join(s0), ln_join(s1)};
         team_sum<G>(s, buf[flip]);
-        const float c1 = s[0] * inv, c2 = s[1] * inv;
-        E *dx = static_cast<E *>(p.out) + row * p.D;
+        // dx = r d - r c1 - xh r c2
+        const T c1 = ln_splat<T>(-s[0] * inv * r), c2 = ln_splat<T>(-s[1] * inv * r);
+        E *dx = static_cast<E *>(p.out) + row * p.D + at.rank * VEC;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int c = (k * at.width + at.rank) * VEC;
-            if (live && c < p.D) {
+            const int c = k * at.width * VEC;
+            if (live && (mask >> k & 1)) {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) h[k][i] = r * (d[k][i] - c1 - h[k][i] * c2);
-                st_vec<E, VEC>(dx + c, h[k]);
+                for (int i = 0; i < P; ++i) h[k][i] = ln_fma(h[k][i], c2, ln_fma(d[k][i], r2, c1));
+                *reinterpret_cast<typename Vec<E, VEC>::raw *>(dx + c) = ln_narrow<E, VEC>(h[k]);
             }
         }
     }
@@ -287,7 +379,7 @@ __global__ void __launch_bounds__(ln_max_threads(G), G > 0 ? 4 : 1) ln_bwd_kerne
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
                     const int c = (k * at.width + at.rank) * VEC + i;
-                    if (c < p.D) dst[c] = dw[k][i], dst[p.D + c] = db[k][i];
+                    if (c < p.D) dst[c] = ln_elem(dw[k], i), dst[p.D + c] = ln_elem(db[k], i);
                 }
         }
         __syncthreads();
@@ -300,7 +392,7 @@ __global__ void __launch_bounds__(ln_max_threads(G), G > 0 ? 4 : 1) ln_bwd_kerne
         for (int i = 0; i < VEC; ++i) {
             const int c = (k * at.width + at.rank) * VEC + i;
             if (c < p.D) {
-                float a = dw[k][i], b = db[k][i];
+                float a = ln_elem(dw[k], i), b = ln_elem(db[k], i);
                 for (int t = 0; t < at.kTeams - 1; ++t) {
                     a += share[(size_t)t * 2 * p.D + c];
                     b += share[(size_t)t * 2 * p.D + p.D + c];
@@ -345,7 +437,7 @@ __global__ void __launch_bounds__(kLnReduceCols * kLnReduceRows)
 struct LnTeam {
     int vec, g, k, threads;
 };
-LnTeam ln_team(const LnParams &p, int es) {
+LnTeam ln_team(const LnParams &p, int es, bool bwd) {
     const int v = 16 / es;
     auto fits = [&](int vec) {
         return p.D % vec == 0 && p.x_stride % vec == 0 && (p.dy == nullptr || p.dy_stride % vec == 0);
@@ -355,20 +447,23 @@ LnTeam ln_team(const LnParams &p, int es) {
     // 8 lanes read 128 bytes of 16-byte vectors; narrower ones take a warp for that
     if (vec == v && nv <= 8 * kmax) return {vec, 8, (nv + 7) / 8, kLnThreads};
     if (nv <= 32 * kmax) return {vec, 32, (nv + 31) / 32, kLnThreads};
-    const int k = p.D <= 1024 * kLnBlockElems ? kLnBlockElems / vec : kmax;
+    const int k = p.D <= (bwd ? kLnBwdThreads : kLnFwdThreads) * kLnBlockElems ? kLnBlockElems / vec : kmax;
     return {vec, 0, k, ((nv + k - 1) / k + 31) / 32 * 32};
 }
 int ln_teams(const LnTeam &t) { return t.g > 0 ? kLnThreads / t.g : 1; }
 
 // One instantiation's launch: as many CTAs as the device holds at a time, each walking its rows (the partial
 // rows of a backward pass: at most `most`).
-template <typename E, int VEC, int K, int G>
-cudaError_t ln_run(const LnParams &p, bool bwd, const LnTeam &t, long long most, int *grid, cudaStream_t stream) {
-    using Fwd = LnAhead<E, VEC, K, G, 1>;
-    using Bwd = LnAhead<E, VEC, K, G, 2>;
-    auto *kernel = bwd ? ln_bwd_kernel<E, VEC, K, G> : ln_fwd_kernel<E, VEC, K, G>;
-    size_t smem = bwd ? Bwd::smem(t.threads) : Fwd::smem(t.threads);
-    if (bwd && p.partial) {
+template <typename E, int VEC, int K, int G, int MAXT, bool BWD>
+cudaError_t ln_run(const LnParams &p, const LnTeam &t, long long most, int *grid, cudaStream_t stream) {
+    using Ahead = LnAhead<E, VEC, K, G, BWD ? 2 : 1>;
+    void (*kernel)(LnParams);
+    if constexpr (BWD)
+        kernel = ln_bwd_kernel<E, VEC, K, G, MAXT>;
+    else
+        kernel = ln_fwd_kernel<E, VEC, K, G, MAXT>;
+    size_t smem = Ahead::smem(t.threads);
+    if (BWD && p.partial) {
         const size_t share = (size_t)(ln_teams(t) - 1) * 2 * p.D * sizeof(float);  // at most 15 x 2 x 128 floats
         if (share > smem) smem = share;
     }
@@ -377,17 +472,20 @@ cudaError_t ln_run(const LnParams &p, bool bwd, const LnTeam &t, long long most,
     if (e == cudaSuccess) e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     // asked once per device and number of warps
-    static std::atomic<int> known[2][64][33] = {};
-    std::atomic<int> &fit = known[bwd][dev & 63][t.threads / 32];
+    static std::atomic<int> known[64][33] = {};
+    std::atomic<int> &fit = known[dev & 63][t.threads / 32];
     per_sm = fit.load(std::memory_order_relaxed);
     if (per_sm == 0) {
-        const int largest = static_cast<int>(bwd ? Bwd::smem(ln_max_threads(G)) : Fwd::smem(ln_max_threads(G)));
+        const int largest = static_cast<int>(Ahead::smem(MAXT));
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, largest > 48 * 1024 ? largest : 48 * 1024);
         if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, t.threads, smem);
         if (e != cudaSuccess) return e;
         if (per_sm < 1) return cudaErrorInvalidConfiguration;
         fit.store(per_sm, std::memory_order_relaxed);
     }
+    // A backward CTA's partial row costs as much as one or two rows of its own, so CTA teams take about 512 threads an
+    // SM (1,024 where only registers hold the next row): at 4,099 x 1,001 fp32 all that fit took 25.8 us.
+    if (BWD && G == 0) per_sm = std::min(per_sm, std::max(1, (Ahead::kAsync ? 512 : 1024) / t.threads));
     long long n = (p.rows + ln_teams(t) - 1) / ln_teams(t);
     if (n > (long long)n_sm * per_sm) n = (long long)n_sm * per_sm;
     if (n > most) n = most;
@@ -395,31 +493,35 @@ cudaError_t ln_run(const LnParams &p, bool bwd, const LnTeam &t, long long most,
     kernel<<<*grid, t.threads, smem, stream>>>(p);
     return cudaGetLastError();
 }
-template <typename E, int VEC> cudaError_t ln_run_v(const LnParams &p, bool bwd, const LnTeam &t, long long most, int *grid,
-                                                     cudaStream_t s) {
-    constexpr int KM = kLnElems / VEC, KH = kLnElems / 2 / VEC;
-    static_assert(KH * VEC == kLnBlockElems, "half the elements");
-    if (t.g == 0)
-        return t.k <= KH ? ln_run<E, VEC, KH, 0>(p, bwd, t, most, grid, s) : ln_run<E, VEC, KM, 0>(p, bwd, t, most, grid, s);
+template <typename E, int VEC, bool BWD> cudaError_t ln_run_v(const LnParams &p, const LnTeam &t, long long most, int *grid,
+                                                                  cudaStream_t s) {
+    constexpr int KM = kLnElems / VEC, KH = kLnBlockElems / VEC, FEW = BWD ? kLnBwdThreads : kLnFwdThreads;
+    if (t.g == 0) {
+        if (t.k <= KH) return ln_run<E, VEC, KH, 0, FEW, BWD>(p, t, most, grid, s);
+        return t.threads <= FEW ? ln_run<E, VEC, KM, 0, FEW, BWD>(p, t, most, grid, s)
+                                : ln_run<E, VEC, KM, 0, kLnMostThreads, BWD>(p, t, most, grid, s);
+    }
     if constexpr (VEC == 16 / static_cast<int>(sizeof(E))) {
         if (t.g == 8)
-            return t.k <= KH ? ln_run<E, VEC, KH, 8>(p, bwd, t, most, grid, s) : ln_run<E, VEC, KM, 8>(p, bwd, t, most, grid, s);
+            return t.k <= KH ? ln_run<E, VEC, KH, 8, kLnThreads, BWD>(p, t, most, grid, s)
+                             : ln_run<E, VEC, KM, 8, kLnThreads, BWD>(p, t, most, grid, s);
     }
-    return t.k <= KH ? ln_run<E, VEC, KH, 32>(p, bwd, t, most, grid, s) : ln_run<E, VEC, KM, 32>(p, bwd, t, most, grid, s);
+    return t.k <= KH ? ln_run<E, VEC, KH, 32, kLnThreads, BWD>(p, t, most, grid, s)
+                     : ln_run<E, VEC, KM, 32, kLnThreads, BWD>(p, t, most, grid, s);
 }
-template <typename E> cudaError_t ln_run_e(const LnParams &p, bool bwd, const LnTeam &t, long long most, int *grid,
-                                                     cudaStream_t s) {
-    if (t.vec == 16 / static_cast<int>(sizeof(E))) return ln_run_v<E, 16 / static_cast<int>(sizeof(E))>(p, bwd, t, most, grid, s);
+template <typename E, bool BWD> cudaError_t ln_run_e(const LnParams &p, long long most, int *grid, cudaStream_t s) {
+    constexpr int V = 16 / static_cast<int>(sizeof(E));
+    const LnTeam t = ln_team(p, sizeof(E), BWD);
+    if (t.vec == V) return ln_run_v<E, V, BWD>(p, t, most, grid, s);
     if constexpr (sizeof(E) == 2) {
-        if (t.vec == 2) return ln_run_v<E, 2>(p, bwd, t, most, grid, s);
+        if (t.vec == 2) return ln_run_v<E, 2, BWD>(p, t, most, grid, s);
     }
-    return ln_run_v<E, 1>(p, bwd, t, most, grid, s);
+    return ln_run_v<E, 1, BWD>(p, t, most, grid, s);
 }
-cudaError_t ln_launch(const LnParams &p, bool bwd, int dtype, long long most, int *grid, cudaStream_t stream) {
-    const LnTeam t = ln_team(p, dtype == 0 ? 4 : 2);
-    if (dtype == 0) return ln_run_e<float>(p, bwd, t, most, grid, stream);
-    if (dtype == 1) return ln_run_e<__half>(p, bwd, t, most, grid, stream);
-    return ln_run_e<__nv_bfloat16>(p, bwd, t, most, grid, stream);
+template <bool BWD> cudaError_t ln_launch(const LnParams &p, int dtype, long long most, int *grid, cudaStream_t stream) {
+    if (dtype == 0) return ln_run_e<float, BWD>(p, most, grid, stream);
+    if (dtype == 1) return ln_run_e<__half, BWD>(p, most, grid, stream);
+    return ln_run_e<__nv_bfloat16, BWD>(p, most, grid, stream);
 }
 
 // Most partial rows of a backward pass: eight CTAs on each of 152 SMs for rows that a warp holds, fewer the more
@@ -435,7 +537,7 @@ long long ln_partial_rows(long long rows, int D) {
 cudaError_t launch_layernorm(const LnProblem &q, cudaStream_t stream) {
     const LnParams p{q.x, q.x_stride, nullptr, 0, q.weight, q.bias, q.eps, q.rows, q.D, q.out, q.mean, q.rstd, nullptr};
     int grid = 0;
-    return ln_launch(p, false, q.dtype, 1LL << 30, &grid, stream);
+    return ln_launch<false>(p, q.dtype, 1LL << 30, &grid, stream);
 }
 
 size_t layernorm_bwd_workspace(long long rows, int D) { return (size_t)ln_partial_rows(rows, D) * 2 * D * sizeof(float); }
@@ -445,7 +547,7 @@ cudaError_t launch_layernorm_bwd(const LnProblem &q, const void *dy, long long d
     const LnParams p{q.x, q.x_stride, dy, dy_stride, q.weight, nullptr, 0.f, q.rows, q.D, q.out, q.mean, q.rstd,
                      (dweight || dbias) ? static_cast<float *>(workspace) : nullptr};
     int grid = 0;
-    const cudaError_t e = ln_launch(p, true, q.dtype, ln_partial_rows(q.rows, q.D), &grid, stream);
+    const cudaError_t e = ln_launch<true>(p, q.dtype, ln_partial_rows(q.rows, q.D), &grid, stream);
     if (e != cudaSuccess || !p.partial) return e;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at;
