@@ -407,8 +407,20 @@ gtr_status_t gtr_ssm_step(const void *x, long long x_stride, const void *delta, 
 gtr_status_t gtr_swiglu_ffn_fwd(const void *x, long long x_stride, const void *w_gate, const void *w_value,
                                 long long M, int D, int F, gtr_dtype_t dtype, void *out, cudaStream_t stream);
 
-/* Bytes of workspace gtr_swiglu_ffn_bwd needs on the current device. */
+/* Bytes of workspace gtr_swiglu_ffn_bwd needs on the current device (dG and dV,
+ * and the partial tiles of the sums that it cuts between CTA pairs there). */
 size_t gtr_swiglu_ffn_bwd_workspace_bytes(long long M, int D, int F);
+
+/* How gtr_swiglu_ffn_bwd deals the products behind dG and dV on a device with
+ * n_sm SMs (n_sm >= 2): *columns of a tile (128 to 512, 256 rows), *cut 0 when
+ * every tile's sum stays with one CTA pair, 1 when dW's, 2 when dx's too are cut
+ * between pairs, in blocks of 64 terms.  Pair i takes the blocks w_start[i] ..
+ * w_start[i + 1] - 1 of dW's tiles (dw_gate's and dw_value's 256-row tiles below one another,
+ * then the next columns), with *cut 2 also x_start[i] .. of dx's; min(pairs + 1,
+ * cap) entries are written (either array may be NULL).  Returns the number of
+ * pairs, or -1 for invalid arguments.  Host arithmetic only: no device is used. */
+int gtr_swiglu_ffn_bwd_plan(long long M, int D, int F, int n_sm, int *columns, int *cut, int *w_start,
+                            int *x_start, int cap);
 
 /* Backward pass of gtr_swiglu_ffn_fwd for the gradient dout [M, F at dout_stride]
  * of its output; the projections G = x Wg^T and V = x Wv^T are computed again:

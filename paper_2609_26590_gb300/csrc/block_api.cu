@@ -118,6 +118,8 @@ gtr_status_t ssm(const void *x, long long x_stride, const void *delta, long long
     return done(step ? gtr::launch_ssm_step(p, stream) : gtr::launch_ssm(p, stream));
 }
 
+constexpr long long kMaxTmaStride = 1LL << 38;  // elements: a tensor map's strides end at 2^40 bytes
+
 // Shape rules of the feed-forward step: TMA wants rows of 16-byte multiples.
 gtr_status_t check_ffn(long long M, int D, int F, int dtype) {
     if (M < 0 || M > kMaxTokens || D < 8 || F < 8 || D % 8 || F % 8 || !dtype_ok(dtype)) return GTR_ERR_INVALID_ARG;
@@ -216,7 +218,7 @@ gtr_status_t gtr_swiglu_ffn_fwd(const void *x, long long x_stride, const void *w
                                 int D, int F, gtr_dtype_t dtype, void *out, cudaStream_t stream) {
     const gtr_status_t st = check_ffn(M, D, F, dtype);
     if (st != GTR_OK) return st;
-    if (!strided(M, x_stride, D) || x_stride % 8) return GTR_ERR_INVALID_ARG;
+    if (!strided(M, x_stride, D) || x_stride % 8 || x_stride > kMaxTmaStride) return GTR_ERR_INVALID_ARG;
     if (M == 0) return GTR_OK;
     if (!x || !w_gate || !w_value || !out || !at16(x) || !at16(w_gate) || !at16(w_value) || !at16(out))
         return GTR_ERR_INVALID_ARG;
@@ -233,13 +235,21 @@ size_t gtr_swiglu_ffn_bwd_workspace_bytes(long long M, int D, int F) {
     return gtr::ffn_bwd_workspace(M, D, F);
 }
 
+int gtr_swiglu_ffn_bwd_plan(long long M, int D, int F, int n_sm, int *columns, int *cut, int *w_start, int *x_start,
+                            int cap) {
+    if (check_ffn(M, D, F, GTR_F16) != GTR_OK || M == 0 || n_sm < 2 || !columns || !cut || cap < 0) return -1;
+    return gtr::ffn_bwd_plan(M, D, F, n_sm, columns, cut, w_start, x_start, cap);
+}
+
 gtr_status_t gtr_swiglu_ffn_bwd(const void *dout, long long dout_stride, const void *x, long long x_stride,
                                 const void *w_gate, const void *w_value, long long M, int D, int F, gtr_dtype_t dtype,
                                 void *dx, void *dw_gate, void *dw_value, void *workspace, size_t workspace_bytes,
                                 cudaStream_t stream) {
     const gtr_status_t st = check_ffn(M, D, F, dtype);
     if (st != GTR_OK) return st;
-    if (!strided(M, x_stride, D) || x_stride % 8 || !strided(M, dout_stride, F) || dout_stride % 8) return GTR_ERR_INVALID_ARG;
+    if (!strided(M, x_stride, D) || x_stride % 8 || x_stride > kMaxTmaStride || !strided(M, dout_stride, F) ||
+        dout_stride % 8 || dout_stride > kMaxTmaStride)
+        return GTR_ERR_INVALID_ARG;
     if (!dw_gate || !dw_value || !at16(dw_gate) || !at16(dw_value) || !at(workspace, 256)) return GTR_ERR_INVALID_ARG;
     const size_t nw = (size_t)F * D * 2;
     if (M == 0) {  // sums over no tokens

@@ -509,7 +509,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGradThreads, 1) ffn
         GradWalk walk(p, pair);
         GradItem item;
         while (walk.next(p, pairs, &item)) {
-            const bool ok = mbar_wait(&bars.acc_full, tile & 1, abort, kFfnWaitNs);
+            // the whole sum's time: 4 us a block and the limit of one wait (a sum over 10^9 tokens takes seconds)
+            const bool ok = mbar_wait(&bars.acc_full, tile & 1, abort, kFfnWaitNs + 4000ull * (item.k1 - item.k0));
             if (!__all_sync(0xffffffffu, ok)) {
                 if (lane == 0) give_up();
                 break;
@@ -861,6 +862,18 @@ cudaError_t launch_ffn(const FfnProblem &q, void *out, cudaStream_t stream) {
     FfnParams p;
     if (!ffn_params(q, p) || !ffn_map(&p.o[0], out, q.dtype, q.M, q.F, q.F, 32, 32)) return cudaErrorInvalidValue;
     return ffn_launch<kFwd>(p, q.dtype, n_sm, stream);
+}
+
+int ffn_bwd_plan(long long M, int D, int F, int n_sm, int *columns, int *cut, int *w_start, int *x_start, int cap) {
+    GradPlan g;
+    if (!ffn_grad_plan(M, D, F, n_sm, &g)) return -1;
+    *columns = g.n_cols;
+    *cut = g.x_cut ? 2 : g.cut ? 1 : 0;
+    for (int i = 0; i <= g.pairs && i < cap; ++i) {
+        if (w_start) w_start[i] = g.w_start[i];
+        if (x_start) x_start[i] = g.x_cut ? g.x_start[i] : 0;
+    }
+    return g.pairs;
 }
 
 size_t ffn_bwd_workspace(long long M, int D, int F) {

@@ -182,6 +182,9 @@ cudaError_t launch_ffn(const FfnProblem &p, void *out, cudaStream_t stream);
 size_t ffn_bwd_workspace(long long M, int D, int F);
 cudaError_t launch_ffn_bwd(const FfnProblem &p, const void *dout, long long dout_stride, void *dx, void *dw_gate,
                            void *dw_value, void *workspace, cudaStream_t stream);
+// How the weights' and tokens' gradients are dealt on a device with n_sm SMs (gtr_swiglu_ffn_bwd_plan): the CTA pairs,
+// or -1.
+int ffn_bwd_plan(long long M, int D, int F, int n_sm, int *columns, int *cut, int *w_start, int *x_start, int cap);
 // Status word of its bounded waits (kStatusTimeout).
 cudaError_t read_and_clear_ffn_status(unsigned int *status);
 

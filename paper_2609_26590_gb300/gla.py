@@ -115,6 +115,8 @@ def load(path: Optional[str] = None):
         lib.gtr_swiglu_ffn_fwd.argtypes = [vp, ll, vp, vp, ll, ci, ci, ci, vp, vp]
         lib.gtr_swiglu_ffn_bwd_workspace_bytes.restype = st
         lib.gtr_swiglu_ffn_bwd_workspace_bytes.argtypes = [ll, ci, ci]
+        lib.gtr_swiglu_ffn_bwd_plan.restype = ci
+        lib.gtr_swiglu_ffn_bwd_plan.argtypes = [ll] + [ci] * 3 + [ctypes.POINTER(ci)] * 4 + [ci]
         lib.gtr_swiglu_ffn_bwd.restype = ci
         lib.gtr_swiglu_ffn_bwd.argtypes = [vp, ll, vp, ll, vp, vp, ll, ci, ci, ci, vp, vp, vp, vp, st, vp]
         if path is None:
@@ -724,6 +726,19 @@ def swiglu_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_value: torch.Tensor, out
 def swiglu_ffn_backward_workspace_bytes(M: int, D: int, F: int) -> int:
     """Device workspace ``swiglu_ffn_backward`` needs for M tokens."""
     return int(load().gtr_swiglu_ffn_bwd_workspace_bytes(M, D, F))
+
+
+def swiglu_ffn_backward_plan(M: int, D: int, F: int, n_sm: int):
+    """(tile columns, cut, w_start, x_start) of the products behind dG and dV on a device with ``n_sm`` SMs, through
+    ``gtr_swiglu_ffn_bwd_plan`` (host arithmetic only): cut 0 for whole tiles, 1 with dW's sums cut, 2 with dx's too."""
+    lib = load()
+    cap = n_sm // 2 + 1
+    columns, cut = ctypes.c_int(0), ctypes.c_int(0)
+    w, x = (ctypes.c_int * cap)(), (ctypes.c_int * cap)()
+    pairs = lib.gtr_swiglu_ffn_bwd_plan(M, D, F, n_sm, ctypes.byref(columns), ctypes.byref(cut), w, x, cap)
+    if pairs < 0:
+        raise ValueError(f"gtr_swiglu_ffn_bwd_plan returned {pairs}")
+    return columns.value, cut.value, list(w[:pairs + 1]), list(x[:pairs + 1])
 
 
 def swiglu_ffn_backward(dout: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_value: torch.Tensor,

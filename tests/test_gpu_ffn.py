@@ -55,7 +55,14 @@ def _check_forward(x, wg, wv, out, what):
 
 
 SHAPES = [(1, 8, 8), (1, 64, 128), (3, 72, 200), (7, 16, 136), (31, 128, 64), (64, 200, 120), (128, 64, 128), (129, 96, 264),
-          (255, 192, 256), (256, 384, 512), (257, 136, 1000), (600, 320, 72), (1000, 1024, 40), (20, 2048, 640), (2000, 264, 2304)]
+          (255, 192, 256), (256, 384, 512), (257, 136, 1000), (600, 320, 72), (1000, 1024, 40), (20, 2048, 640), (2000, 264, 2304),
+          # up to eight tokens: each instantiation, inputs wider than a CTA takes at once, many channels
+          (2, 264, 40), (4, 2056, 72), (5, 496, 136), (6, 8, 16), (8, 4104, 24), (1, 5000, 96), (2, 64, 20000), (9, 64, 72),
+          # the weights stay resident over several tiles; the gradients' tiles of 384 and 512 columns, whole and cut
+          (5000, 384, 520), (3000, 448, 1200), (300, 1544, 2600), (20000, 384, 264), (2500, 2040, 1000),
+          # ... and dx's sums cut with and without dW's
+          (276, 32, 3160), (1662, 56, 3088), (2016, 248, 5456), (65, 608, 3208), (67, 848, 4224), (4032, 1960, 88),
+          (3196, 976, 64)]
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
