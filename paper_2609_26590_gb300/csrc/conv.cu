@@ -69,36 +69,39 @@ __global__ void __launch_bounds__(kConvThreads, 3) conv_kernel(const __grid_cons
     // registers, one batch ahead.
     constexpr bool ASYNC = sizeof(Raw) >= 4;
     extern __shared__ uint4 conv_smem[];
-    Raw *slots = reinterpret_cast<Raw *>(conv_smem) + threadIdx.y * blockDim.x + threadIdx.x;
-    const int stride = blockDim.x * blockDim.y;
+    const uint32_t pitch = static_cast<uint32_t>(sizeof(Raw)) * blockDim.x * blockDim.y;  // between a thread's slots
+    const uint32_t slots = ptx::smem_u32(conv_smem) + static_cast<uint32_t>(sizeof(Raw)) * (threadIdx.y * blockDim.x + threadIdx.x);
     Raw in[kConvBatch];
-    ScanPos ahead, pos;
-    ahead.set(p.grid, s0);
-    pos = ahead;
-    int fetched = s0, slot = 0;
+    ScanPos start;
+    start.set(p.grid, s0);
+    ScanWalk<const E> ahead(p.grid, start, x, p.x_stride);
+    ScanWalk<E> to(p.grid, start, out, p.E);
+    int fetched = s0;
+    uint32_t slot = slots;
     auto fetch = [&] {
 #pragma unroll
-        for (int k = 0; k < kConvBatch; ++k)
-            if (fetched + k < s1) {
-                const E *src = x + (long long)ahead.t * p.x_stride;
-                if constexpr (!ASYNC)
-                    in[k] = *reinterpret_cast<const Raw *>(src);
-                else if constexpr (sizeof(Raw) == 16)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
-                                     ptx::smem_u32(slots + (slot * kConvBatch + k) * stride)),
-                                 "l"(src)
-                                 : "memory");
-                else
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(
-                                     ptx::smem_u32(slots + (slot * kConvBatch + k) * stride)),
-                                 "l"(src), "n"(sizeof(Raw))
-                                 : "memory");
-                ahead.next(p.grid);
+        for (int k = 0; k < kConvBatch; ++k) {
+            const bool live = fetched + k < s1;
+            if constexpr (!ASYNC) {
+                if (live) in[k] = *reinterpret_cast<const Raw *>(ahead.at);
+            } else if constexpr (sizeof(Raw) == 16) {
+                asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(
+                                 slot + k * pitch),
+                             "l"(ahead.at), "r"(static_cast<uint32_t>(live))
+                             : "memory");
+            } else {
+                asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], %3;\n\t}" ::"r"(
+                                 slot + k * pitch),
+                             "l"(ahead.at), "r"(static_cast<uint32_t>(live)), "n"(sizeof(Raw))
+                             : "memory");
             }
+            ahead.next();
+        }
         fetched += kConvBatch;
         if constexpr (ASYNC) {
             asm volatile("cp.async.commit_group;" ::: "memory");
-            slot = slot + 1 == kConvDepth ? 0 : slot + 1;
+            slot += kConvBatch * pitch;
+            if (slot == slots + kConvDepth * kConvBatch * pitch) slot = slots;
         }
     };
 #pragma unroll
@@ -146,38 +149,60 @@ __global__ void __launch_bounds__(kConvThreads, 3) conv_kernel(const __grid_cons
         }
         return Vec<E, VEC>::pack(f);
     };
+    auto output = [&](const Raw &r, f2(&a)[P]) {  // takes in one input: its sum
+#pragma unroll
+        for (int j = 0; j + 1 < W; ++j)
+#pragma unroll
+            for (int i = 0; i < P; ++i) win[j][i] = win[j + 1][i];
+        widen(r, win[W - 1]);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            a[i] = bias[i];
+#pragma unroll
+            for (int j = 0; j < W; ++j) a[i] = fma2(w[j][i], win[j][i], a[i]);
+        }
+    };
     for (int s = s0; s < s1; s += kConvBatch) {
         Raw now[kConvBatch];
         if constexpr (ASYNC) asm volatile("cp.async.wait_group %0;" ::"n"(kConvDepth - 1) : "memory");
 #pragma unroll
         for (int k = 0; k < kConvBatch; ++k) {
             if constexpr (ASYNC)
-                now[k] = slots[(slot * kConvBatch + k) * stride];  // (what no copy wrote is not used)
+                now[k] = *reinterpret_cast<const Raw *>(reinterpret_cast<const uint8_t *>(conv_smem) +
+                                                        (slot - ptx::smem_u32(conv_smem) + k * pitch));  // (what no copy wrote is not used)
             else
                 now[k] = in[k];
         }
         fetch();
+        if (s + kConvBatch <= s1) {
+            f2 a[kConvBatch][P];
 #pragma unroll
-        for (int k = 0; k < kConvBatch; ++k) {
-            if (s + k >= s1) break;
-#pragma unroll
-            for (int j = 0; j + 1 < W; ++j)
-#pragma unroll
-                for (int i = 0; i < P; ++i) win[j][i] = win[j + 1][i];
-            widen(now[k], win[W - 1]);
-            f2 a[P];
-#pragma unroll
-            for (int i = 0; i < P; ++i) {
-                a[i] = bias[i];
-#pragma unroll
-                for (int j = 0; j < W; ++j) a[i] = fma2(w[j][i], win[j][i], a[i]);
-            }
+            for (int k = 0; k < kConvBatch; ++k) output(now[k], a[k]);
             if (p.silu) {
 #pragma unroll
-                for (int i = 0; i < P; ++i) a[i] = silu_pair<E>(a[i]);
+                for (int k = 0; k < kConvBatch; ++k)
+#pragma unroll
+                    for (int i = 0; i < P; ++i) a[k][i] = silu_pair<E>(a[k][i]);
             }
-            *reinterpret_cast<Raw *>(out + (long long)pos.t * p.E) = narrow(a);
-            pos.next(p.grid);
+#pragma unroll
+            for (int k = 0; k < kConvBatch; ++k) {
+                *reinterpret_cast<Raw *>(to.at) = narrow(a[k]);
+                to.next();
+            }
+        } else {  // the last positions of a sequence
+#pragma unroll
+            for (int k = 0; k + 1 < kConvBatch; ++k) {
+                if (s + k < s1) {
+                    f2 a[P];
+                    output(now[k], a);
+                    if (p.silu) {
+#pragma unroll
+                        for (int i = 0; i < P; ++i) a[i] = silu_pair<E>(a[i]);
+                    }
+                    *reinterpret_cast<Raw *>(to.at) = narrow(a);
+                    to.next();
+                }
+            }
         }
     }
     if constexpr (ASYNC) asm volatile("cp.async.wait_all;" ::: "memory");

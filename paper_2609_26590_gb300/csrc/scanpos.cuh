@@ -40,4 +40,28 @@ struct ScanPos {
     }
 };
 
+// The same walk as an address: `stride` elements a token.
+template <typename P> struct ScanWalk {
+    P *at;
+    long long on, over;  // to the next position, and from the last one of a column (column orders)
+    int left, run;       // positions before that
+    __device__ __forceinline__ ScanWalk(const ScanGrid &g, const ScanPos &pos, P *base, long long stride) {
+        at = base + pos.t * stride;
+        const long long one = (g.order & 1) ? -1 : 1;
+        if (g.order & 2) {
+            on = one * g.gw * stride;
+            over = one * (1 - static_cast<long long>(g.T - g.gw)) * stride;
+            left = (g.order & 1) ? pos.row : g.gh.d - 1 - pos.row;
+            run = g.gh.d - 1;
+        } else {
+            on = over = one * stride;
+            left = run = 0x7fffffff;
+        }
+    }
+    __device__ __forceinline__ void next() {
+        at += left > 0 ? on : over;
+        left = left > 0 ? left - 1 : run;
+    }
+};
+
 }  // namespace gtr
