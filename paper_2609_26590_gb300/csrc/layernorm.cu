@@ -12,6 +12,11 @@
 // it visits; the next row's loads are issued before the current row's sums.  Each
 // CTA then adds its teams' shares in shared memory and writes one partial row; a second
 // kernel adds the partial rows in a fixed order (no atomics: the same bits every time).
+//
+// Measured on a GB300 (graph replays over inputs larger than L2; TB/s of the bytes that have to move, the
+// measured copy runs at 6.78): backward 51,200 x 384 bf16 28.5 us (4.1 TB/s; 25 the rows, 4 the column sums),
+// 4,099 x 1,001 fp32 16.4 us (3.0 TB/s; no vector divides its rows), forward 1,600 x 192 fp16 2.4 us (a launch).
+// With the row's loads inside the loop and no row ahead the first two took 48.9 and 47 us.
 #include <cuda_runtime.h>
 
 #include <algorithm>

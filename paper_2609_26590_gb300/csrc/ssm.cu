@@ -15,6 +15,13 @@
 // walk yields each segment's end state from zero and its sum of dt (the segment's decay is exp(A sum dt)), the
 // warps fold the earlier segments of their CTA and then the earlier CTAs' totals out of their shared memory, and
 // the second walk starts from the fold.
+// What bounds it: instructions.  A token and 32 channels take a warp about 110 with the readout and 95 without, 38 of
+// both to the hardware's power and reciprocal (8 lanes a cycle and scheduler) and 60 to the FMA pipe (a packed
+// operation holds it two cycles).  Measured on a GB300: 8 x 80 x 80 x 768 x 16 bf16, row order, 305 us (207 us were
+// its instructions issued without a gap; the bytes alone would take 47), one 40 x 40 x 384 fp16 image 19.7 us (its
+// 56 segments of 32 positions wait for their own results).  Not kept: four lanes a channel that exchange
+// readouts, no segments (521 us: 1.3 warps a scheduler, 3.8 cycles an instruction), barriers of a CTA whose warps
+// share the rows (617 us).
 #include <cuda_runtime.h>
 
 #include <mutex>
@@ -469,26 +476,28 @@ __global__ void __launch_bounds__(32 * kSsmMaxWarps, kSsmMinCtas) ssm_kernel(con
 
 // One token of every sequence.  Memory-bound: the states are read and written once.  Four states a
 // thread in one 16-byte access, N / 4 neighbouring lanes a channel (N / 4 a power of two), and the same
-// channels of kStepSeqs sequences, whose loads are issued together; A, D and the bias are read once for them.
+// channels of four sequences, whose loads are issued together; A, D and the bias are read once for them.
+// What a channel has once, its step size and its output, is worked out by one of its lanes a sequence (q, and with
+// two lanes q + 2, with one all four) and passed on by shuffles.
+// Measured on a GB300: 256 sequences x 1,536 x 16 bf16 11.3 us (4.7 TB/s, 70 % of the measured copy); every lane working
+// out all step sizes 13.9 us, one sequence a thread 16.7 us.
 constexpr int kStepSeqs = 4;
 template <typename E, int LPC, bool QUADS>  // QUADS: B and C start on four elements
 __global__ void __launch_bounds__(256, 4) ssm_step_kernel(const __grid_constant__ SsmParams p) {
     using Four = typename Vec<E, 4>::raw;
+    constexpr int OWN = LPC >= 4 ? 1 : 4 / LPC, EACH = LPC >= 4 ? 4 : LPC;  // sequences of a lane: q % EACH + EACH j
     const int per = p.E * LPC;  // threads a sequence
     const int blocks = (per + 255) / 256;
     const int group = blockIdx.x / blocks, i = (blockIdx.x - group * blocks) * 256 + threadIdx.x;
     const bool live = i < per;
     const int c = live ? i / LPC : 0, q = i % LPC, b0 = group * kStepSeqs;
     float4 h[kStepSeqs];
-    E u[kStepSeqs], v[kStepSeqs], zv[kStepSeqs];
     Four bq[kStepSeqs], cq[kStepSeqs];
+    E u[OWN], v[OWN], zv[OWN];
 #pragma unroll
     for (int k = 0; k < kStepSeqs; ++k) {
         const int b = b0 + k < p.B ? b0 + k : p.B - 1;  // (the last sequence again: not stored)
         h[k] = *reinterpret_cast<const float4 *>(p.init + ((long long)b * p.E + c) * (4 * LPC) + 4 * q);
-        u[k] = static_cast<const E *>(p.x)[(long long)b * p.x_stride + c];
-        v[k] = static_cast<const E *>(p.delta)[(long long)b * p.delta_stride + c];
-        if (p.z) zv[k] = static_cast<const E *>(p.z)[(long long)b * p.z_stride + c];
         const E *Bm = static_cast<const E *>(p.Bm) + (long long)b * p.b_stride + 4 * q;
         const E *C = static_cast<const E *>(p.C) + (long long)b * p.c_stride + 4 * q;
         if constexpr (QUADS) {
@@ -501,32 +510,72 @@ __global__ void __launch_bounds__(256, 4) ssm_step_kernel(const __grid_constant_
             cq[k] = Vec<E, 4>::pack(g);
         }
     }
+#pragma unroll
+    for (int j = 0; j < OWN; ++j) {
+        const int k = q % EACH + EACH * j, b = b0 + k < p.B ? b0 + k : p.B - 1;
+        u[j] = static_cast<const E *>(p.x)[(long long)b * p.x_stride + c];
+        v[j] = static_cast<const E *>(p.delta)[(long long)b * p.delta_stride + c];
+        if (p.z) zv[j] = static_cast<const E *>(p.z)[(long long)b * p.z_stride + c];
+    }
     const float4 a = *reinterpret_cast<const float4 *>(p.A + (long long)c * (4 * LPC) + 4 * q);
     const float av[4] = {a.x * kLog2e, a.y * kLog2e, a.z * kLog2e, a.w * kLog2e};
     const float bias = p.bias ? p.bias[c] : 0.f, skip = p.D ? p.D[c] : 0.f;
+    float dt[OWN], du[OWN];
+#pragma unroll
+    for (int j = 0; j < OWN; ++j) {
+        dt[j] = to_f32(v[j]) + bias;
+        if (p.softplus) dt[j] = softplus(dt[j]);
+        du[j] = dt[j] * to_f32(u[j]);
+    }
+    float y[kStepSeqs];
 #pragma unroll
     for (int k = 0; k < kStepSeqs; ++k) {
-        const int b = b0 + k;
-        const float uk = to_f32(u[k]);
-        float dt = to_f32(v[k]) + bias;
-        if (p.softplus) dt = softplus(dt);
-        const float du = dt * uk, hv[4] = {h[k].x, h[k].y, h[k].z, h[k].w};
-        float n[4], bv[4], cv[4], y = 0.f;
+        float d = dt[k / EACH], w = du[k / EACH];
+        if constexpr (LPC > 1) {
+            const int from = (threadIdx.x & 31 & ~(LPC - 1)) + k % EACH;
+            d = __shfl_sync(0xffffffffu, d, from);
+            w = __shfl_sync(0xffffffffu, w, from);
+        }
+        const float hv[4] = {h[k].x, h[k].y, h[k].z, h[k].w};
+        float n[4], bv[4], cv[4];
         Vec<E, 4>::unpack(bq[k], bv);
         Vec<E, 4>::unpack(cq[k], cv);
+        y[k] = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            n[j] = fmaf(exp2_hw(dt * av[j]), hv[j], du * bv[j]);
-            y = fmaf(cv[j], n[j], y);
+            n[j] = fmaf(exp2_hw(d * av[j]), hv[j], w * bv[j]);
+            y[k] = fmaf(cv[j], n[j], y[k]);
         }
-        if (live && b < p.B)
-            *reinterpret_cast<float4 *>(p.state + ((long long)b * p.E + c) * (4 * LPC) + 4 * q) = make_float4(n[0], n[1], n[2], n[3]);
+        if (live && b0 + k < p.B)
+            *reinterpret_cast<float4 *>(p.state + ((long long)(b0 + k) * p.E + c) * (4 * LPC) + 4 * q) =
+                make_float4(n[0], n[1], n[2], n[3]);
+    }
+    // sums over the channel's lanes: each ends with those of its own sequences
 #pragma unroll
-        for (int o = LPC / 2; o > 0; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
-        if (live && b < p.B && q == 0) {
-            y = fmaf(skip, uk, y);
-            if (p.z) y *= silu<E>(to_f32(zv[k]));
-            static_cast<E *>(p.out)[(long long)b * p.E + c] = from_f32<E>(y);
+    for (int o = LPC / 2; o >= 4; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < kStepSeqs; ++k) y[k] += __shfl_xor_sync(0xffffffffu, y[k], o);
+    auto halve = [&](float &even, float &odd, int o) {  // lanes with bit o of q keep `odd`
+        const bool hi = q & o;
+        const float keep = hi ? odd : even, send = hi ? even : odd;
+        even = keep + __shfl_xor_sync(0xffffffffu, send, o);
+    };
+    if constexpr (LPC >= 4) {
+        halve(y[0], y[2], 2);
+        halve(y[1], y[3], 2);
+        halve(y[0], y[1], 1);
+    } else if constexpr (LPC == 2) {
+        halve(y[0], y[1], 1);
+        halve(y[2], y[3], 1);
+        y[1] = y[2];
+    }
+#pragma unroll
+    for (int j = 0; j < OWN; ++j) {
+        const int k = q % EACH + EACH * j;
+        if (live && b0 + k < p.B && q < EACH) {
+            float r = fmaf(skip, to_f32(u[j]), y[j]);
+            if (p.z) r *= silu<E>(to_f32(zv[j]));
+            static_cast<E *>(p.out)[(long long)(b0 + k) * p.E + c] = from_f32<E>(r);
         }
     }
 }
