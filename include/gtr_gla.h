@@ -1,7 +1,7 @@
 /*
  * gtr_gla.h -- C ABI of the GB300 (sm_103a) chunkwise gated-linear-attention
  * forward: the token mixer of GTR ("GTR: Gated Token Recurrence for Efficient
- * Dense Prediction").
+ * Dense Prediction"), and of the operators around it in a block.
  *
  * Operation (Sec. 3.1, "Key-only gated recurrence"; value-side decay fixed to
  * one, Sec. 3.1 and App. C.3), per batch b and head h, along one scan order:

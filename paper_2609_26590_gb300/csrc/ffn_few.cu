@@ -151,7 +151,7 @@ template <typename E> cudaError_t few_run_m(const FewParams &p, int n_sm, cudaSt
 }  // namespace
 
 // One and two tokens stream the weights; more cost the CUDA cores arithmetic that the tensor-core kernel's tile does
-// not notice, so that up to eight run here only while its fixed time (two hundred blocks of K on few SMs) is longer.
+// not notice, so that up to eight run here only while its fixed time (few tiles, each a long sum, on few SMs) is longer.
 // Measured in us, here and there, at F D = 1.3 million: four tokens 4.4 and 12.3, eight 5.0 and 12.3; at 11.5 million: two
 // 11.3 and 18, four 19.4 and 18, eight 29.3 and 18.
 bool ffn_few(long long M, int D, int F) {

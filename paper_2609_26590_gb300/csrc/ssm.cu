@@ -15,10 +15,10 @@
 // walk yields each segment's end state from zero and its sum of dt (the segment's decay is exp(A sum dt)), the
 // warps fold the earlier segments of their CTA and then the earlier CTAs' totals out of their shared memory, and
 // the second walk starts from the fold.
-// What bounds it: instructions.  A token and 32 channels take a warp about 110 with the readout and 95 without, 38 of
-// both to the hardware's power and reciprocal (8 lanes a cycle and scheduler) and 60 to the FMA pipe (a packed
-// operation holds it two cycles).  Measured on a GB300: 8 x 80 x 80 x 768 x 16 bf16, row order, 305 us (207 us were
-// its instructions issued without a gap; the bytes alone would take 47), one 40 x 40 x 384 fp16 image 19.7 us (its
+// What bounds it: instructions.  A token and 32 channels take 194 over both walks, 37 of them the hardware's power and
+// reciprocal (8 lanes a cycle and scheduler) and 94 on the FMA pipe (a packed operation holds it two cycles).
+// Measured on a GB300: 8 x 80 x 80 x 768 x 16 bf16, row order, 305 us (2.66 of 4 instructions a cycle and SM, FMA
+// pipe 52 %; the bytes alone would take 47), one 40 x 40 x 384 fp16 image 19.7 us (its
 // 56 segments of 32 positions wait for their own results).  Not kept: four lanes a channel that exchange
 // readouts, no segments (521 us: 1.3 warps a scheduler, 3.8 cycles an instruction), barriers of a CTA whose warps
 // share the rows (617 us).
@@ -627,8 +627,8 @@ struct SsmFit {
 
 // The cheapest cut by what a launch takes: its clusters in waves of those the device places, a token kIssue[r]
 // cycles an instruction with r warps on a scheduler (warps take turns, one alone waits for its own results; measured
-// on a GB300 at 20 to 10,000 positions and 12 to 2,048 channel groups), two walks of 205 instructions a token and 16 states
-// against one of 115, and the start, the folds and the cluster's barriers beside them.
+// on a GB300 at 20 to 10,000 positions and 12 to 2,048 channel groups), two walks of 205 units a token and 16 states
+// against one of 115 (about their instructions, fitted with kIssue), and the start, the folds and the cluster's barriers beside them.
 SsmPlan ssm_plan(long long units, int T, const SsmFit &fit) {
     static const float kIssue[5] = {0.f, 2.25f, 2.95f, 4.2f, 5.5f};
     const int blocks = (T - 1) / kSsmBlock + 1;
