@@ -96,6 +96,8 @@ gtr_status_t ssm(const void *x, long long x_stride, const void *delta, long long
     if (st != GTR_OK) return st;
     const long long T = (long long)grid_h * grid_w, n = (long long)B * T, es = esize(dtype);
     if (N < 1 || N > 64 || (softplus != 0 && softplus != 1)) return GTR_ERR_INVALID_ARG;
+    const int group = N <= 16 ? 32 : N <= 32 ? 16 : 8;  // channels a warp walks
+    if (!step && (long long)B * ((E + group - 1) / group) > (1 << 27)) return GTR_ERR_INVALID_ARG;
     if (!strided(n, x_stride, E) || !strided(n, delta_stride, E) || !strided(n, b_stride, N) || !strided(n, c_stride, N) ||
         (z && !strided(n, z_stride, E)))
         return GTR_ERR_INVALID_ARG;

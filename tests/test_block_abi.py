@@ -183,3 +183,12 @@ def test_row_strides():
             _row_stride(bad, "t")
     assert _row_stride(torch.zeros(5, 1), "t") == 1
     assert _row_stride(torch.zeros(0, 7), "t") == 7
+
+
+@pytest.mark.parametrize("E,N,per", [(8, 16, 32), (16, 32, 16), (8, 64, 8), (33, 16, 32)])
+def test_ssm_refuses_more_groups_than_documented(lib, E, N, per):
+    far = 1 << 44  # nothing overlaps
+    groups = -(-E // per)
+    B = (1 << 27) // groups + 1
+    assert _ssm(lib, x=far, dl=2 * far, A=3 * far, b=4 * far, c=5 * far, D=None, z=None, bias=None, out=6 * far, fs=None,
+                xs=E, ds=E, bs=N, cs=N, B=B, gh=1, gw=1, E=E, N=N) == INVALID
