@@ -5,12 +5,12 @@
 //
 // Products of persistent kernels on CTA pairs (tcgen05 cta_group::2): 64-deep blocks of both operands
 // arrive by TMA in 128-byte-swizzled shared memory (rows and columns outside the tensors as zeros), one
-// warp issues the MMAs, and eight warps empty the TMEM accumulator.
+// warp issues the MMAs, and eight or sixteen warps empty the TMEM accumulator.
 //   ffn_kernel<kFwd>  both projections of 128 channels as one 256 x 256 tile (gate columns from the even CTA's
 //                     weights, value columns from the odd one's), SiLU and the product in registers, H stored; the
 //                     next tile fills a second accumulator meanwhile
 //   ffn_kernel<kAct>  the same projections again (nothing of M x F is kept between the passes), dH read beside
-//                     them, dG and dV stored in the inputs' type: they are operands of the next products,
+//                     them, dG and dV stored (rows padded to 32 bytes) in the inputs' type: they are operands of the next products,
 //                     which the tensor cores take in 16 bits (half a step of rounding each)
 //   ffn_grad_kernel   dX = [dG dV] [Wg; Wv], the weights read along F (MN-major), and dWg, dWv, both operands read
 //                     along the tokens (MN-major), as one launch whose tiles are dealt so that the pairs end
@@ -19,8 +19,8 @@
 //
 // Measured on a GB300 (bf16 peak of the library's largest products: 1,969 TFLOP/s): 51,200 x 384 x 1,536 bf16 forward 72 to
 // 74 us (1,650 TFLOP/s); backward 8,192 x 2,048 x 5,632 bf16 626 to 636 us (1,780 to 1,810 TFLOP/s; the tensor pipe
-// active 84 % of kAct's 215 us and 94 % of the gradients' 395), 12,797 x 384 x 2,304 fp16 115 us (45, 62 and 8 us: kAct
-// moves 187 MB beside its short sums, the gradients' kernel ends within a tile of its even share, the cut sums).
+// active 84 % of kAct's 215 us and 94 % of the gradients' 395), 12,797 x 384 x 2,304 fp16 114 us (45, 63 and 6 us: kAct
+// moves 190 MB beside its short sums, the gradients' kernel ends within a tile of its even share, the cut sums).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -59,7 +59,7 @@ constexpr uint64_t kFfnWaitNs = 1000000000ull;
 constexpr int kResident = 6;       // blocks of D up to which a tile's weights stay in shared memory
 // Stages: A and B, or with resident weights A alone.
 constexpr int ffn_stages(int mode, bool res) { return mode == kAct ? (res ? 4 : 5) : 6; }
-constexpr int ffn_boxes(int mode) { return mode == kAct ? 2 : 1; }  // staging boxes of a warp: H, or dG, and dH, then dV
+constexpr int ffn_boxes(int mode) { return mode == kAct ? 2 : 1; }  // boxes of a warp: H, or dH of this tile and the next
 constexpr int ffn_box_at(int mode, bool res) {
     return res ? (kResident + ffn_stages(mode, true)) * kStageA : ffn_stages(mode, false) * kStageBytes;
 }
@@ -69,8 +69,10 @@ constexpr size_t ffn_smem(int mode, bool res) {
 
 struct FfnParams {
     CUtensorMap a, b[2];  // tokens; gate and value weights
-    CUtensorMap o[2];     // H, or dG and dV
-    CUtensorMap dh;       // kAct
+    CUtensorMap o;        // kFwd: H
+    CUtensorMap dh;       // kAct: dH
+    void *act[2];         // kAct: dG and dV, at act_stride
+    long long act_stride;
     FastDiv tm;           // tiles down the rows
     int tiles;
     int nk;               // 64-deep blocks of a tile
@@ -79,7 +81,7 @@ struct FfnParams {
 };
 
 struct FfnBars {
-    uint64_t full[6], empty[6], acc_full[2], acc_empty[2], dh[16];
+    uint64_t full[6], empty[6], acc_full[2], acc_empty[2], dh[2][16];
     uint64_t w_full[kResident], w_empty[kResident];  // resident weights
     uint32_t tmem, abort;
 };
@@ -123,7 +125,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
     if (threadIdx.x == 0) {
         for (int i = 0; i < S; ++i) mbar_init(&bars.full[i], 1), mbar_init(&bars.empty[i], 1);
         for (int i = 0; i < 2; ++i) mbar_init(&bars.acc_full[i], 1), mbar_init(&bars.acc_empty[i], 32);
-        for (int i = 0; i < 16; ++i) mbar_init(&bars.dh[i], 1);
+        for (int i = 0; i < 16; ++i) mbar_init(&bars.dh[0][i], 1), mbar_init(&bars.dh[1][i], 1);
         for (int i = 0; i < kResident; ++i) mbar_init(&bars.w_full[i], 1), mbar_init(&bars.w_empty[i], 1);
         bars.abort = 0;
         fence_mbar_init();
@@ -224,16 +226,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
         uint8_t *box = smem + ffn_box_at(MODE, RES) + (size_t)w * BOXES * kBox;
         const uint32_t lanes = static_cast<uint32_t>(sub * 32) << 16;
         const uint32_t acc_empty = map_to_cta(smem_u32(&bars.acc_empty[0]), 0);  // the even CTA's, 8 bytes apart
-        // dH of the next tile arrives while its accumulator is filled
-        auto load_dh = [&](int tile) {
+        // kAct: dH arrives in two boxes, a tile ahead; dG and dV leave the registers as whole 32-byte sectors.  (Stored
+        // from the boxes, which dH then had to wait for, the kernel took 49.0 us instead of 45.2 at 12,797 x 384 x 2,304;
+        // dH loaded into registers 52.)
+        auto load_dh = [&](int tile, uint32_t slot) {
             if (tile >= tile1) return;
             const int n = fdiv(tile, p.tm), m = tile - n * p.tm.d;
-            mbar_arrive_expect_tx(&bars.dh[w], kBox);
-            tma_load_2d(box + kBox, &p.dh, &bars.dh[w], n * 128 + quarter * 32,
+            mbar_arrive_expect_tx(&bars.dh[slot][w], kBox);
+            tma_load_2d(box + slot * kBox, &p.dh, &bars.dh[slot][w], n * 128 + quarter * 32,
                         m * kTileM + static_cast<int>(rank) * 128 + sub * 32);
         };
         if constexpr (MODE == kAct) {
-            if (lane == 0) load_dh(tile0);
+            if (lane == 0) load_dh(tile0, 0), load_dh(tile0 + step, 1);
         }
         uint32_t acc = 0;
         for (int tile = tile0; tile < tile1; tile += step, ++acc) {
@@ -241,7 +245,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
             const uint32_t buf = acc & 1;
             const int row0 = m * kTileM + static_cast<int>(rank) * 128 + sub * 32, col0 = n * 128 + quarter * 32;
             bool ok = mbar_wait(&bars.acc_full[buf], (acc >> 1) & 1, abort, kFfnWaitNs);
-            if constexpr (MODE == kAct) ok = mbar_wait(&bars.dh[w], acc & 1, nullptr, kFfnWaitNs) && ok;
+            if constexpr (MODE == kAct) ok = mbar_wait(&bars.dh[buf][w], (acc >> 1) & 1, nullptr, kFfnWaitNs) && ok;
             if (!__all_sync(0xffffffffu, ok)) {
                 if (lane == 0) give_up();
                 break;
@@ -259,15 +263,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
                 if (MODE == kFwd) bulk_wait_read();                // the box of the tile before has been stored
             }
             if (MODE == kFwd) __syncwarp();
+            const long long out = (row0 + lane) * p.act_stride + col0;  // kAct
+            uint32_t o0[8], o1[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {  // 16 bytes: eight columns; 64-byte swizzle
-                uint4 *at = reinterpret_cast<uint4 *>(box + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4));
-                uint4 *at_dh = reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(at) + kBox);
-                uint32_t in[4], o0[4], o1[4];
+                uint4 *at = reinterpret_cast<uint4 *>(box + (MODE == kAct ? buf * kBox : 0) + lane * 64 +
+                                                      ((j ^ ((lane >> 1) & 3)) << 4));
+                uint32_t in[4];
                 if constexpr (MODE == kAct) {
-                    const uint4 d = *at_dh;
+                    const uint4 d = *at;
                     in[0] = d.x, in[1] = d.y, in[2] = d.z, in[3] = d.w;
                 }
+                const int half = MODE == kAct ? 4 * (j & 1) : 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const f2 z = pack2(g[8 * j + 2 * i], g[8 * j + 2 * i + 1]);
@@ -281,30 +288,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) ffn_
                         // dG = dH V s (1 + G (1 - s)), dV = dH s G
                         const float2 dg = unpack2(mul2(mul2(ds, y), fma2(z, fma2(sg, pack2(-1.f, -1.f), one), one)));
                         const float2 dv = unpack2(mul2(ds, z));
-                        o0[i] = pack16<E>(dg.x, dg.y);
-                        o1[i] = pack16<E>(dv.x, dv.y);
+                        o0[half + i] = pack16<E>(dg.x, dg.y);
+                        o1[half + i] = pack16<E>(dv.x, dv.y);
                     }
                 }
-                *at = make_uint4(o0[0], o0[1], o0[2], o0[3]);
-                if constexpr (MODE == kAct) *at_dh = make_uint4(o1[0], o1[1], o1[2], o1[3]);  // dV where dH was
+                if constexpr (MODE == kFwd) {
+                    *at = make_uint4(o0[0], o0[1], o0[2], o0[3]);
+                } else if (j & 1) {
+                    // (columns up to act_stride exist: F rounded up to 16)
+                    if (row0 + lane < p.rows && col0 + 8 * (j - 1) < p.cols) {
+                        st_global_32b(static_cast<E *>(p.act[0]) + out + 8 * (j - 1), o0);
+                        st_global_32b(static_cast<E *>(p.act[1]) + out + 8 * (j - 1), o1);
+                    }
+                }
             }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                if (row0 < p.rows && col0 < p.cols) {
-                    tma_store_2d(&p.o[0], box, col0, row0);
-                    if constexpr (MODE == kAct) tma_store_2d(&p.o[1], box + kBox, col0, row0);
+            if constexpr (MODE == kFwd) {
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0 && row0 < p.rows && col0 < p.cols) {
+                    tma_store_2d(&p.o, box, col0, row0);
                     bulk_commit();
                 }
-                if constexpr (MODE == kAct) {
-                    bulk_wait_read();  // both boxes have been stored: the next dH may come
-                    load_dh(tile + step);
-                }
+            } else {
+                __syncwarp();  // every lane has read its dH
+                if (lane == 0) load_dh(tile + 2 * step, buf);
             }
             __syncwarp();
         }
-        if constexpr (MODE == kAct) {  // after giving up: the last dH box may still be on its way
-            if (lane == 0 && tile0 + static_cast<int>(acc) * step < tile1) mbar_wait(&bars.dh[w], acc & 1, nullptr, kFfnWaitNs);
+        if constexpr (MODE == kAct) {  // after giving up: dH of this tile and the next may still be on their way
+            for (uint32_t a = acc; a < acc + 2; ++a)
+                if (lane == 0 && tile0 + static_cast<int>(a) * step < tile1)
+                    mbar_wait(&bars.dh[a & 1][w], (a >> 1) & 1, nullptr, kFfnWaitNs);
         }
         if (lane == 0) bulk_wait_all();
     }
@@ -811,7 +825,9 @@ bool ffn_grad_plan(long long M, int D, int F, int n_sm, GradPlan *out) {
 size_t grad_partial_bytes(const GradPlan &g) {
     return g.cut ? (size_t)(g.x_cut ? 4 : 2) * g.pairs * kTileM * g.n_cols * sizeof(float) : 0;
 }
-size_t act_bytes(long long M, int F) { return ((size_t)M * F * 2 + 255) / 256 * 256; }
+// dG and dV in the workspace: rows of whole 32-byte sectors
+int act_stride(int F) { return (F + 15) / 16 * 16; }
+size_t act_bytes(long long M, int F) { return ((size_t)M * act_stride(F) * 2 + 255) / 256 * 256; }
 
 template <typename E> cudaError_t grad_launch(const GradParams &p, const GradPlan &g, void *dx, void *dw_gate, void *dw_value,
                                               cudaStream_t stream) {
@@ -865,7 +881,7 @@ cudaError_t launch_ffn(const FfnProblem &q, void *out, cudaStream_t stream) {
     const cudaError_t e = sm_count(&n_sm);
     if (e != cudaSuccess) return e;
     FfnParams p;
-    if (!ffn_params(q, p) || !ffn_map(&p.o[0], out, q.dtype, q.M, q.F, q.F, 32, 32)) return cudaErrorInvalidValue;
+    if (!ffn_params(q, p) || !ffn_map(&p.o, out, q.dtype, q.M, q.F, q.F, 32, 32)) return cudaErrorInvalidValue;
     return ffn_launch<kFwd>(p, q.dtype, n_sm, stream);
 }
 
@@ -915,18 +931,19 @@ cudaError_t launch_ffn_bwd(const FfnProblem &q, const void *dout, long long dout
     if (e != cudaSuccess) return e;
     char *dg = static_cast<char *>(workspace), *dv = dg + act_bytes(q.M, q.F);
     FfnParams p;
-    if (!ffn_params(q, p) || !ffn_map(&p.o[0], dg, q.dtype, q.M, q.F, q.F, 32, 32) ||
-        !ffn_map(&p.o[1], dv, q.dtype, q.M, q.F, q.F, 32, 32) || !ffn_map(&p.dh, dout, q.dtype, q.M, q.F, dout_stride, 32, 32))
+    const int as = act_stride(q.F);
+    if (!ffn_params(q, p) || !ffn_map(&p.dh, dout, q.dtype, q.M, q.F, dout_stride, 32, 32))
         return cudaErrorInvalidValue;
     GradPlan g;
     if (!last_plan(q.M, q.D, q.F, n_sm, &g)) return cudaErrorInvalidValue;
+    p.act[0] = dg, p.act[1] = dv, p.act_stride = as;
     if ((e = ffn_launch<kAct>(p, q.dtype, n_sm, stream)) != cudaSuccess) return e;
 
     GradParams r;
     std::memset(&r, 0, sizeof(r));
-    if (!ffn_map(&r.ax[0], dg, q.dtype, q.M, q.F, q.F, 128) || !ffn_map(&r.ax[1], dv, q.dtype, q.M, q.F, q.F, 128) ||
+    if (!ffn_map(&r.ax[0], dg, q.dtype, q.M, q.F, as, 128) || !ffn_map(&r.ax[1], dv, q.dtype, q.M, q.F, as, 128) ||
         !ffn_map(&r.bx[0], q.w_gate, q.dtype, q.F, q.D, q.D, 64) || !ffn_map(&r.bx[1], q.w_value, q.dtype, q.F, q.D, q.D, 64) ||
-        !ffn_map(&r.aw[0], dg, q.dtype, q.M, q.F, q.F, 64) || !ffn_map(&r.aw[1], dv, q.dtype, q.M, q.F, q.F, 64) ||
+        !ffn_map(&r.aw[0], dg, q.dtype, q.M, q.F, as, 64) || !ffn_map(&r.aw[1], dv, q.dtype, q.M, q.F, as, 64) ||
         !ffn_map(&r.bw, q.x, q.dtype, q.M, q.D, q.x_stride, 64) || !ffn_map(&r.o[0], dx, q.dtype, q.M, q.D, q.D, 32) ||
         !ffn_map(&r.o[1], dw_gate, q.dtype, q.F, q.D, q.D, 32) || !ffn_map(&r.o[2], dw_value, q.dtype, q.F, q.D, q.D, 32))
         return cudaErrorInvalidValue;
