@@ -8,12 +8,13 @@
 // alignment does not allow that) and walks a strip of scan positions with the last W inputs
 // in registers; the scan order is in the walk's addresses.
 //
-// Measured on a GB300: 32 x 40 x 40 x 768 bf16, column order, 35.3 us (4.4 TB/s of the bytes that have to move, 66 % of
+// Measured on a GB300: 32 x 40 x 40 x 768 bf16, column order, 30.9 us (5.1 TB/s of the bytes that have to move, 75 % of
 // the measured copy); bound by the copies in flight and the issue of SiLU's instructions together.  Loads in
 // registers, four positions ahead: 60 us; addresses formed from the position for each token: 48 us.  Single tokens
 // of 256 x 1,536 fp16: 3.3 us.
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "elem.cuh"
@@ -25,7 +26,7 @@ namespace gtr {
 namespace {
 
 constexpr int kConvThreads = 256;
-constexpr int kConvStrip = 32;  // most scan positions a thread walks
+constexpr int kConvStrip = 128; // most scan positions a thread walks
 constexpr int kConvBatch = 4;   // positions loaded at a time
 constexpr int kConvDepth = 4;   // batches in flight
 
@@ -257,31 +258,64 @@ template <typename E, int VEC> size_t conv_smem_bytes(int threads) {  // at most
     return raw >= 4 ? raw * kConvBatch * kConvDepth * threads : 0;
 }
 
+// CTAs of one instantiation that an SM holds, asked once per device and number of warps.
+template <typename E, int VEC, int W> cudaError_t conv_fit(int threads, int *per_sm) {
+    static std::atomic<int> known[64][kConvThreads / 32 + 1] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const int warps = (threads + 31) / 32;
+    std::atomic<int> &fit = known[dev & 63][warps];
+    *per_sm = fit.load(std::memory_order_relaxed);
+    if (*per_sm > 0) return cudaSuccess;
+    auto *kernel = conv_kernel<E, VEC, W>;
+    const size_t most = conv_smem_bytes<E, VEC>(kConvThreads);
+    if (most > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most));
+    if (e == cudaSuccess)
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(per_sm, kernel, 32 * warps, conv_smem_bytes<E, VEC>(32 * warps));
+    if (e != cudaSuccess) return e;
+    if (*per_sm < 1) return cudaErrorInvalidConfiguration;
+    fit.store(*per_sm, std::memory_order_relaxed);
+    return cudaSuccess;
+}
+
+// The scan positions of a strip, by what the busiest SM takes for its rounds of CTAs: a start of 13 positions' latency
+// (taps, the window, the first copies), then each position that latency or the CTAs' bytes, whichever is more
+// (cta_bytes: warps x bytes a lane; 57 of them take one latency).  Fitted to 13 problems at 20 lengths on a GB300.  In us,
+// against strips of 32 halved until there were 1,024 threads an SM: bf16 32 x 1,600 x 768 30.9 (35.4), 128 x 1,600 x 768
+// 103 (119); fp32 32 x 1,600 x 768 62 (66.7); fp16 4 x 1,600 x 768 8.7 (12.3), 4 x 400 x 1,536 5.8 (7.2), 300 x 49 x 768
+// 11.6 (15.0), 16 x 784 x 500 11.0 (11.3); slower among 20 sizes only 1 x 100,000 x 64, 10.9 (10.6).
+int conv_strip(int B, int T, int by, int ny, int cta_bytes, int per_sm, int n_sm) {
+    int best = kConvBatch;
+    float least = 0.f;
+    for (int strip = kConvBatch; strip <= kConvStrip; strip += strip < 64 ? kConvBatch : 2 * kConvBatch) {
+        const long long ctas = ((long long)B * ((T - 1) / strip + 1) + by - 1) / by * ny, n = (ctas + n_sm - 1) / n_sm;
+        const float walk = static_cast<float>(strip < T ? strip : T);
+        auto round = [&](long long held) { return 13.f + walk * std::max(1.f, held * cta_bytes / 57.f); };
+        const float t = n / per_sm * round(per_sm) + (n % per_sm ? round(n % per_sm) : 0.f);
+        if (strip == kConvBatch || t < least) least = t, best = strip;
+        if (strip >= T) break;
+    }
+    return best;
+}
+
 template <typename E, int VEC, int W> cudaError_t conv_run(ConvParams &p, bool step, int n_sm, cudaStream_t stream) {
     const int nv = (p.E + VEC - 1) / VEC;
     const int ny = (nv + kConvThreads - 1) / kConvThreads;
     const int bx = (nv + ny - 1) / ny, by = kConvThreads / bx;  // bx <= 256
-    // strips as long as they still leave the SMs twice their threads
-    p.strip = kConvStrip;
-    while (p.strip > kConvBatch && (long long)p.B * ((p.grid.T - 1) / p.strip + 1) * nv < 1024LL * n_sm) p.strip /= 2;
-    p.strips = (p.grid.T - 1) / p.strip + 1;
+    p.strip = p.strips = 1;
+    if (!step) {
+        int per_sm = 0;
+        const cudaError_t e = conv_fit<E, VEC, W>(bx * by, &per_sm);
+        if (e != cudaSuccess) return e;
+        const int raw = static_cast<int>(sizeof(typename Vec<E, VEC>::raw));
+        p.strip = conv_strip(p.B, p.grid.T, by, ny, (bx * by + 31) / 32 * (raw < 4 ? 4 : raw), per_sm, n_sm);
+        p.strips = (p.grid.T - 1) / p.strip + 1;
+    }
     p.items = (long long)p.B * p.strips;
     const long long rows = step ? p.B : p.items, gx = (rows + by - 1) / by;
     if (gx > 0x7fffffffLL || ny > 65535) return cudaErrorInvalidValue;
     const dim3 grid(static_cast<unsigned>(gx), ny), block(bx, by);
-    if (!step && conv_smem_bytes<E, VEC>(kConvThreads) > 48 * 1024) {
-        static std::atomic<unsigned long long> set_on_devices(0);
-        int dev = 0;
-        cudaError_t e = cudaGetDevice(&dev);
-        if (e != cudaSuccess) return e;
-        const unsigned long long bit = 1ull << (dev & 63);
-        if (!(set_on_devices.load(std::memory_order_relaxed) & bit)) {
-            e = cudaFuncSetAttribute(conv_kernel<E, VEC, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     static_cast<int>(conv_smem_bytes<E, VEC>(kConvThreads)));
-            if (e != cudaSuccess) return e;
-            set_on_devices.fetch_or(bit);
-        }
-    }
     if (step)
         conv_step_kernel<E, VEC, W><<<grid, block, 0, stream>>>(p);
     else
