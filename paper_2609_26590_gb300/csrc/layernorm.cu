@@ -146,6 +146,10 @@ template <typename E, int VEC, int K, int G, int NT> struct LnAhead {
                 return make_float4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]));
             else
                 return make_uint4(w[0], w[1], w[2], w[3]);
+        } else if constexpr (sizeof(Raw) == 8) {
+            uint2 w;
+            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w.x), "=r"(w.y) : "r"(slot + (n * K + k) * pitch) : "memory");
+            return w;
         } else {
             uint32_t w;
             asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(slot + (n * K + k) * pitch) : "memory");
@@ -447,7 +451,13 @@ LnTeam ln_team(const LnParams &p, int es, bool bwd) {
     auto fits = [&](int vec) {
         return p.D % vec == 0 && p.x_stride % vec == 0 && (p.dy == nullptr || p.dy_stride % vec == 0);
     };
-    const int vec = fits(v) ? v : es == 2 && fits(2) ? 2 : 1;
+    int vec = fits(v) ? v : es == 2 && fits(4) ? 4 : es == 2 && fits(2) ? 2 : 1;
+    // a warp's row in 8-byte vectors where those leave its lanes fewer elements than 16-byte ones: three of 4 instead of
+    // two of 8 for 257 to 384 (backward, us: 1,600 x 384 6.5 against 7.9, 12,800 x 384 13.0 against 14.3, 51,200 x 384 29.4
+    // against 29.3, 51,200 x 320 27.8 against 26.9); widths of 4 and not 8 take them too (forward, 4-byte vectors in
+    // brackets: 51,200 x 300 16.5 (22.2), 20,000 x 1,004 24.6 (32.8), 8,000 x 2,052 23.1 (29.7))
+    auto lane_elems = [&](int of) { return ((p.D + of - 1) / of + 31) / 32 * of; };
+    if (vec == 8 && lane_elems(8) <= kLnElems && lane_elems(4) < lane_elems(8)) vec = 4;
     const int nv = (p.D + vec - 1) / vec, kmax = kLnElems / vec;
     // 8 lanes read 128 bytes of 16-byte vectors; narrower ones take a warp for that
     if (vec == v && nv <= 8 * kmax) return {vec, 8, (nv + 7) / 8, kLnThreads};
@@ -511,6 +521,9 @@ template <typename E, int VEC, bool BWD> cudaError_t ln_run_v(const LnParams &p,
             return t.k <= KH ? ln_run<E, VEC, KH, 8, kLnThreads, BWD>(p, t, most, grid, s)
                              : ln_run<E, VEC, KM, 8, kLnThreads, BWD>(p, t, most, grid, s);
     }
+    if constexpr (VEC == 4) {
+        if (t.k == 3) return ln_run<E, VEC, 3, 32, kLnThreads, BWD>(p, t, most, grid, s);
+    }
     return t.k <= KH ? ln_run<E, VEC, KH, 32, kLnThreads, BWD>(p, t, most, grid, s)
                      : ln_run<E, VEC, KM, 32, kLnThreads, BWD>(p, t, most, grid, s);
 }
@@ -519,6 +532,7 @@ template <typename E, bool BWD> cudaError_t ln_run_e(const LnParams &p, long lon
     const LnTeam t = ln_team(p, sizeof(E), BWD);
     if (t.vec == V) return ln_run_v<E, V, BWD>(p, t, most, grid, s);
     if constexpr (sizeof(E) == 2) {
+        if (t.vec == 4) return ln_run_v<E, 4, BWD>(p, t, most, grid, s);
         if (t.vec == 2) return ln_run_v<E, 2, BWD>(p, t, most, grid, s);
     }
     return ln_run_v<E, 1, BWD>(p, t, most, grid, s);

@@ -60,7 +60,8 @@ def _check_forward(x, w, b, out, mean, rstd, what):
 
 # every team (8 lanes, a warp, a CTA), full and ragged vectors, single elements and single rows
 SHAPES = [(1, 1), (3, 2), (5, 7), (1, 64), (33, 64), (17, 127), (130, 128), (7, 130), (1600, 192), (77, 384), (2, 512),
-          (9, 513), (65, 1000), (41, 1001), (3, 4096), (2, 4099), (5, 8192), (1, 16384), (2, 16383)]
+          (9, 513), (65, 1000), (41, 1001), (3, 4096), (2, 4099), (5, 8192), (1, 16384), (2, 16383),
+          (130, 300), (65, 320), (33, 380), (9, 460), (41, 1004), (3, 8196), (1, 16380), (19, 4), (7, 12)]
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
