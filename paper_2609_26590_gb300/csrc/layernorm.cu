@@ -14,8 +14,8 @@
 // kernel adds the partial rows in a fixed order (no atomics: the same bits every time).
 //
 // Measured on a GB300 (graph replays over inputs larger than L2; TB/s of the bytes that have to move, the
-// measured copy runs at 6.78): backward 51,200 x 384 bf16 28.5 us (4.1 TB/s; 25 the rows, 4 the column sums),
-// 4,099 x 1,001 fp32 16.4 us (3.0 TB/s; no vector divides its rows), forward 1,600 x 192 fp16 2.4 us (a launch).
+// measured copy runs at 6.78): backward 51,200 x 384 bf16 28.1 us (4.2 TB/s; the rows
+// bound by a warp's chain of wait, sums over its lanes and stores: 51,200 x 192, half the bytes, takes 18.7), 4,099 x 1,001 fp32 16.4 us (3.0 TB/s; no vector divides its rows), forward 1,600 x 192 fp16 2.4 us (a launch).
 // With the row's loads inside the loop and no row ahead the first two took 48.9 and 47 us.
 #include <cuda_runtime.h>
 
@@ -301,11 +301,12 @@ __global__ void __launch_bounds__(MAXT, 1) ln_fwd_kernel(const __grid_constant__
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-template <typename E, int VEC, int K, int G, int MAXT>
+// R: rows that a team takes at a time.  Two overlap their chains of a wait, sums over the lanes and stores.
+template <typename E, int VEC, int K, int G, int MAXT, int R>
 __global__ void __launch_bounds__(MAXT, G > 0 ? 4 : 1) ln_bwd_kernel(const __grid_constant__ LnParams p) {
     using Ahead = LnAhead<E, VEC, K, G, 2>;
     extern __shared__ float4 ln_smem[];
-    __shared__ float buf[2][2][32];
+    __shared__ float buf[2][2 * R][32];
     const LnPlace<G> at;
     const float inv = 1.f / static_cast<float>(p.D);
     const long long step = (long long)gridDim.x * at.kTeams;
@@ -322,56 +323,70 @@ __global__ void __launch_bounds__(MAXT, G > 0 ? 4 : 1) ln_bwd_kernel(const __gri
     };
 #pragma unroll
     for (int i = 0; i < Ahead::kDepth; ++i) fetch();
-    float next_m = 0.f, next_r = 0.f;
-    auto stats = [&](long long row) {
-        if (row < p.rows) next_m = p.mean[row], next_r = p.rstd[row];
+    float next_m[R] = {}, next_r[R] = {};
+    auto stats = [&](int q, long long row) {
+        if (row < p.rows) next_m[q] = p.mean[row], next_r[q] = p.rstd[row];
     };
-    stats((long long)blockIdx.x * at.kTeams + at.team);
+#pragma unroll
+    for (int q = 0; q < R; ++q) stats(q, (long long)blockIdx.x * at.kTeams + at.team + q * step);
     using T = LnNum<VEC>;
     constexpr int P = kLnNums<VEC>;
     T w[K][P], dw[K][P] = {}, db[K][P] = {};
 #pragma unroll
     for (int k = 0; k < K; ++k) ln_params<VEC>(p.w, (k * at.width + at.rank) * VEC, p.D, 1.f, w[k]);
     int flip = 0;
-    for (long long base = (long long)blockIdx.x * at.kTeams; base < p.rows; base += step, flip ^= 1) {
-        const long long row = base + at.team;
-        const bool live = row < p.rows;
-        const float m = next_m, r = next_r;
-        stats(row + step);
-        T h[K][P], d[K][P], s0 = 0, s1 = 0;
-        const T minus_m = ln_splat<T>(-m), r2 = ln_splat<T>(r);
-        ahead.ready();
+    for (long long base = (long long)blockIdx.x * at.kTeams; base < p.rows; base += R * step, flip ^= 1) {
+        T h[R][K][P], d[R][K][P];
+        float s[2 * R], rs[R];
+        T r2[R];
+        long long row[R];
+        bool live[R];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const bool in = live && (mask >> k & 1);
-            if (VEC == 1 || in) {  // (a slot that no copy wrote holds anything: xh and dy count as zero)
-                ln_widen<E, VEC>(ahead.get(0, k), h[k]);
-                ln_widen<E, VEC>(ahead.get(1, k), d[k]);
-                if (VEC == 1 && !in) h[k][0] = ln_splat<T>(m), d[k][0] = 0;
+        for (int q = 0; q < R; ++q) {
+            row[q] = base + q * step + at.team;
+            live[q] = row[q] < p.rows;
+            const float m = next_m[q];
+            rs[q] = next_r[q];
+            stats(q, row[q] + R * step);
+            T s0 = 0, s1 = 0;
+            const T minus_m = ln_splat<T>(-m);
+            r2[q] = ln_splat<T>(rs[q]);
+            ahead.ready();
 #pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    h[k][i] = ln_mul(ln_add(h[k][i], minus_m), r2);
-                    dw[k][i] = ln_fma(d[k][i], h[k][i], dw[k][i]);
-                    db[k][i] = ln_add(db[k][i], d[k][i]);
-                    d[k][i] = ln_mul(d[k][i], w[k][i]);
-                    s0 = ln_add(s0, d[k][i]);
-                    s1 = ln_fma(d[k][i], h[k][i], s1);
+            for (int k = 0; k < K; ++k) {
+                const bool in = live[q] && (mask >> k & 1);
+                if (VEC == 1 || in) {  // (a slot that no copy wrote holds anything: xh and dy count as zero)
+                    ln_widen<E, VEC>(ahead.get(0, k), h[q][k]);
+                    ln_widen<E, VEC>(ahead.get(1, k), d[q][k]);
+                    if (VEC == 1 && !in) h[q][k][0] = ln_splat<T>(m), d[q][k][0] = 0;
+#pragma unroll
+                    for (int i = 0; i < P; ++i) {
+                        h[q][k][i] = ln_mul(ln_add(h[q][k][i], minus_m), r2[q]);
+                        dw[k][i] = ln_fma(d[q][k][i], h[q][k][i], dw[k][i]);
+                        db[k][i] = ln_add(db[k][i], d[q][k][i]);
+                        d[q][k][i] = ln_mul(d[q][k][i], w[k][i]);
+                        s0 = ln_add(s0, d[q][k][i]);
+                        s1 = ln_fma(d[q][k][i], h[q][k][i], s1);
+                    }
                 }
             }
+            fetch();
+            s[2 * q] = ln_join(s0), s[2 * q + 1] = ln_join(s1);
         }
-        fetch();
-        float s[2] = {ln_join(s0), ln_join(s1)};
         team_sum<G>(s, buf[flip]);
-        // dx = r d - r c1 - xh r c2
-        const T c1 = ln_splat<T>(-s[0] * inv * r), c2 = ln_splat<T>(-s[1] * inv * r);
-        E *dx = static_cast<E *>(p.out) + row * p.D + at.rank * VEC;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int c = k * at.width * VEC;
-            if (live && (mask >> k & 1)) {
+        for (int q = 0; q < R; ++q) {
+            // dx = r d - r c1 - xh r c2
+            E *dx = static_cast<E *>(p.out) + row[q] * p.D + at.rank * VEC;
+            const T c1 = ln_splat<T>(-s[2 * q] * inv * rs[q]), c2 = ln_splat<T>(-s[2 * q + 1] * inv * rs[q]);
 #pragma unroll
-                for (int i = 0; i < P; ++i) h[k][i] = ln_fma(h[k][i], c2, ln_fma(d[k][i], r2, c1));
-                *reinterpret_cast<typename Vec<E, VEC>::raw *>(dx + c) = ln_narrow<E, VEC>(h[k]);
+            for (int k = 0; k < K; ++k) {
+                const int c = k * at.width * VEC;
+                if (live[q] && (mask >> k & 1)) {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) h[q][k][i] = ln_fma(h[q][k][i], c2, ln_fma(d[q][k][i], r2[q], c1));
+                    *reinterpret_cast<typename Vec<E, VEC>::raw *>(dx + c) = ln_narrow<E, VEC>(h[q][k]);
+                }
             }
         }
     }
@@ -469,12 +484,12 @@ int ln_teams(const LnTeam &t) { return t.g > 0 ? kLnThreads / t.g : 1; }
 
 // One instantiation's launch: as many CTAs as the device holds at a time, each walking its rows (the partial
 // rows of a backward pass: at most `most`).
-template <typename E, int VEC, int K, int G, int MAXT, bool BWD>
+template <typename E, int VEC, int K, int G, int MAXT, bool BWD, int R = 1>
 cudaError_t ln_run(const LnParams &p, const LnTeam &t, long long most, int *grid, cudaStream_t stream) {
     using Ahead = LnAhead<E, VEC, K, G, BWD ? 2 : 1>;
     void (*kernel)(LnParams);
     if constexpr (BWD)
-        kernel = ln_bwd_kernel<E, VEC, K, G, MAXT>;
+        kernel = ln_bwd_kernel<E, VEC, K, G, MAXT, R>;
     else
         kernel = ln_fwd_kernel<E, VEC, K, G, MAXT>;
     size_t smem = Ahead::smem(t.threads);
@@ -520,6 +535,19 @@ template <typename E, int VEC, bool BWD> cudaError_t ln_run_v(const LnParams &p,
         if (t.g == 8)
             return t.k <= KH ? ln_run<E, VEC, KH, 8, kLnThreads, BWD>(p, t, most, grid, s)
                              : ln_run<E, VEC, KM, 8, kLnThreads, BWD>(p, t, most, grid, s);
+    }
+    // Two rows at a time: 16-bit elements of which a lane holds at most 8, or 12 and a team walks ten rows and more.  In us,
+    // one row at a time in brackets: 51,200 x 192 18.7 (22.5), x 256 20.8 (24.6), x 384 28.1 (29.8), x 130 19.0 (19.6), 12,800 x
+    // 256 10.9 (11.3), but 3,000 x 256 7.9 (7.6); 12,800 x 384 would take 13.7 (13.0), fp32, which spills, 51,200 x 384 43.6
+    // (40.2), and the forward pass, with fewer warps an SM, 51,200 x 384 17.8 (16.8).
+    if constexpr (BWD && sizeof(E) == 2 && VEC == 4) {
+        int n_sm = 0;
+        const cudaError_t e = sm_count(&n_sm);
+        if (e != cudaSuccess) return e;
+        if (t.k == 3 && p.rows >= 10LL * 16 * n_sm) return ln_run<E, VEC, 3, 32, kLnThreads, BWD, 2>(p, t, most, grid, s);
+    }
+    if constexpr (BWD && sizeof(E) == 2 && VEC > 1) {
+        if (t.k <= KH) return ln_run<E, VEC, KH, 32, kLnThreads, BWD, 2>(p, t, most, grid, s);
     }
     if constexpr (VEC == 4) {
         if (t.k == 3) return ln_run<E, VEC, 3, 32, kLnThreads, BWD>(p, t, most, grid, s);

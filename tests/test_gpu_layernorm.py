@@ -138,7 +138,7 @@ def _check_backward(x, dy, w, mean, rstd, dx, dw, db, what):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
-@pytest.mark.parametrize("rows,D", SHAPES + [(5000, 64), (20000, 24)], ids=lambda v: str(v))
+@pytest.mark.parametrize("rows,D", SHAPES + [(5000, 64), (20000, 24), (24577, 264), (25001, 300), (4867, 256)], ids=lambda v: str(v))
 def test_backward(rows, D, dtype):
     x, dy, w, b = _inputs(rows, D, dtype, 200 + rows + D)
     _, mean, rstd = gla.layernorm(x, w, b, EPS, stats=True)
