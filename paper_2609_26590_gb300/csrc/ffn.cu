@@ -18,9 +18,9 @@
 // Every wait is bounded; a kernel that gives up sets the status word.
 //
 // Measured on a GB300 (bf16 peak of the library's largest products: 1,969 TFLOP/s): 51,200 x 384 x 1,536 bf16 forward 72 to
-// 74 us (1,650 TFLOP/s); backward 8,192 x 2,048 x 5,632 bf16 626 to 636 us (1,780 to 1,810 TFLOP/s; the tensor pipe
-// active 84 % of kAct's 215 us and 94 % of the gradients' 395), 12,797 x 384 x 2,304 fp16 114 us (45, 63 and 6 us: kAct
-// moves 190 MB beside its short sums, the gradients' kernel ends within a tile of its even share, the cut sums).
+// 74 us (1,650 TFLOP/s); backward 8,192 x 2,048 x 5,632 bf16 632 to 656 us (1,730 to 1,800 TFLOP/s; the tensor pipe
+// active 90 % of kAct's 206 us and 94 % of the gradients' 389), 12,797 x 384 x 2,304 fp16 112 to 114 us (45, 63 and 6 us:
+// kAct moves 190 MB beside its short sums, the gradients' kernel ends within a tile of its even share, the cut sums).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 

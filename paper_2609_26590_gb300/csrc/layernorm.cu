@@ -14,7 +14,7 @@
 // kernel adds the partial rows in a fixed order (no atomics: the same bits every time).
 //
 // Measured on a GB300 (graph replays over inputs larger than L2; TB/s of the bytes that have to move, the
-// measured copy runs at 6.78): backward 51,200 x 384 bf16 28.1 us (4.2 TB/s; the rows
+// measured copy runs at 6.78): backward 51,200 x 384 bf16 27.5 to 28.1 us (4.2 TB/s; the rows
 // bound by a warp's chain of wait, sums over its lanes and stores: 51,200 x 192, half the bytes, takes 18.7), 4,099 x 1,001 fp32 16.4 us (3.0 TB/s; no vector divides its rows), forward 1,600 x 192 fp16 2.4 us (a launch).
 // With the row's loads inside the loop and no row ahead the first two took 48.9 and 47 us.
 #include <cuda_runtime.h>
