@@ -6,6 +6,10 @@ fp32 arithmetic moves a value across a rounding border.  Eleven steps round; if 
 values by one step (2 u, u half a step), that is u / 2 in the mean square each, behind gains of up to 2: below
 4 u together.  The training chain compares with 64-bit autograd without those roundings: five of them (the norm's
 output, dG and dV, the step's gradient, the norm's gradient), each u / sqrt(3) or less in the mean square: below 3 u."""
+import pathlib
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -180,3 +184,44 @@ def test_two_streams_at_once():
                 got.append(_block(xs[i], w, 20, 20, i)[0])
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(ref, got))
+
+
+FIRST_CALLS = {
+    "layernorm": "lambda: gla.layernorm(x, v, v, 1e-5)",
+    "layernorm_backward": "lambda: gla.layernorm_backward(x, x, v, s, s)[0]",
+    "causal_conv": "lambda: gla.causal_conv(x[None], w, v, 8, 8)[0]",
+    "causal_conv_step": "lambda: gla.causal_conv_step(x, c, w, v, state_out=c2)[0]",
+    "ssm_scan": "lambda: gla.ssm_scan(x[None], x[None], a, b[None], b[None], 8, 8)[0]",
+    "ssm_step": "lambda: gla.ssm_step(x, x, a, b, b, h, state_out=h2)[0]",
+    "swiglu_ffn": "lambda: gla.swiglu_ffn(x, f, f)",
+    "swiglu_ffn_few": "lambda: gla.swiglu_ffn(x[:1], f, f)",
+    "swiglu_ffn_backward": "lambda: gla.swiglu_ffn_backward(x, x, q, q)[0]",
+}
+
+
+@pytest.mark.parametrize("name", sorted(FIRST_CALLS))
+def test_first_call_captured(name):
+    """The first call of a process inside a capture: what an operator asks the device once is legal there."""
+    code = f"""
+import torch
+from paper_2609_26590_gb300 import gla
+gla.load()
+g = torch.Generator(device="cuda").manual_seed(5)
+def r(*n, dt=torch.float16): return torch.randn(n, device="cuda", generator=g).to(dt)
+x, f, q, b = r(64, 128), r(200, 128) / 11, r(128, 128) / 11, r(64, 16)
+v, s, w, a = torch.rand(128, device="cuda"), torch.rand(64, device="cuda"), r(128, 4, dt=torch.float32), -torch.rand(128, 16, device="cuda")
+c, h = r(64, 3, 128), r(64, 128, 16, dt=torch.float32)
+c2, h2 = torch.empty_like(c), torch.empty_like(h)
+call = {FIRST_CALLS[name]}
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = call()
+graph.replay()
+torch.cuda.synchronize()
+assert torch.equal(out, call()) and bool(torch.isfinite(out.float()).all())
+assert gla.sync_status() == 0
+"""
+    root = pathlib.Path(__file__).resolve().parent.parent
+    run = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0, run.stderr[-2000:]
