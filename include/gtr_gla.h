@@ -320,7 +320,9 @@ gtr_status_t gtr_gla_fwd_lowrank_gate(const void *q, const void *k, const void *
  *   NULL (ones, zeros); out: [n, D] contiguous; mean, rstd: [n] float32 or NULL
  *   (what the backward pass reads).
  * x and out 16-byte aligned; 1 <= D <= 16384; n >= 0 (0 launches nothing);
- * eps >= 0.  D and x_stride multiples of 16 bytes run on 16-byte vectors. */
+ * eps >= 0.  D and x_stride multiples of 16 bytes run on 16-byte vectors.  The
+ * number of rows chooses between kernels that add a row in different orders, so a
+ * row's result can differ in fp32's last bits from that in a call of other n. */
 gtr_status_t gtr_layernorm_fwd(const void *x, long long x_stride, const float *weight, const float *bias,
                                float eps, long long n, int D, gtr_dtype_t dtype, void *out, float *mean,
                                float *rstd, cudaStream_t stream);

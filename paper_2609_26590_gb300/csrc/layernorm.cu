@@ -9,7 +9,8 @@
 // difference of moments), and the row is written once.  A row belongs to a team of threads:
 // 8 lanes, a warp or a whole CTA, whichever keeps a thread at 16 elements or fewer, so that
 // it keeps its share of the weights and, in the backward pass, of dw and db beside them for all rows
-// it visits; the next row's loads are issued before the current row's sums.  Each
+// it visits; the next row's loads are issued before the current row's sums.  Many wide 16-bit rows
+// of the forward pass are held by one warp each instead (ln_fwd_wide_kernel).  Each backward
 // CTA then adds its teams' shares in shared memory and writes one partial row; a second
 // kernel adds the partial rows in a fixed order (no atomics: the same bits every time).
 //
@@ -34,6 +35,7 @@ constexpr int kLnThreads = 128;  // CTA of sub-warp and warp teams
 constexpr int kLnElems = 16;     // elements of a row a thread holds at most
 constexpr int kLnBlockElems = 8; // of a row that a whole CTA holds, as long as the CTA's threads suffice
 // Threads of a CTA team: 64 registers a thread hold 8 elements of the forward pass, the backward pass's take 128.
+constexpr int kLnWideThreads = 256;
 constexpr int kLnFwdThreads = 1024, kLnBwdThreads = 512, kLnMostThreads = 1024;
 
 template <int G> __device__ __forceinline__ float lane_sum(float a) {
@@ -301,6 +303,82 @@ __global__ void __launch_bounds__(MAXT, 1) ln_fwd_kernel(const __grid_constant__
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
+// A row of many elements held by one warp, as stored (up to 256 bytes a lane), so that what a row costs beside its
+// elements is paid by one warp and no barrier is met; the weights lie in shared memory, pieces of four floats in planes
+// that 8 lanes read without a bank conflict.
+template <typename E, int VEC, int K>
+__global__ void __launch_bounds__(kLnWideThreads, K * VEC * sizeof(E) <= 64 ? 4 : K * VEC * sizeof(E) <= 128 ? 3 : 2)
+    ln_fwd_wide_kernel(const __grid_constant__ LnParams p) {
+    constexpr int P = VEC / 2, Q = VEC / 4;
+    using Raw = typename Vec<E, VEC>::raw;
+    extern __shared__ float4 ln_smem[];  // [w, b][Q][32 K]
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    for (int i = threadIdx.x; i < 32 * K * Q; i += blockDim.x) {
+        const int c = i / Q * VEC + i % Q * 4, to = i % Q * 32 * K + i / Q;
+        float w[4], b[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            w[j] = p.w && c + j < p.D ? p.w[c + j] : 1.f;
+            b[j] = p.b && c + j < p.D ? p.b[c + j] : 0.f;
+        }
+        ln_smem[to] = make_float4(w[0], w[1], w[2], w[3]);
+        ln_smem[32 * K * Q + to] = make_float4(b[0], b[1], b[2], b[3]);
+    }
+    __syncthreads();
+    const float inv = 1.f / static_cast<float>(p.D);
+    const uint32_t mask = ln_mask<VEC, K>(lane, 32, p.D);
+    for (long long row = (long long)blockIdx.x * warps + (threadIdx.x >> 5); row < p.rows; row += (long long)gridDim.x * warps) {
+        const E *x = static_cast<const E *>(p.x) + row * p.x_stride + lane * VEC;
+        Raw raw[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (mask >> k & 1) raw[k] = *reinterpret_cast<const Raw *>(x + k * 32 * VEC);
+        f2 sum = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (mask >> k & 1) {
+                f2 v[P];
+                unpack_pairs<E, VEC>(raw[k], v);
+#pragma unroll
+                for (int i = 0; i < P; ++i) sum = add2(sum, v[i]);
+            }
+        const float m = lane_sum<32>(ln_join(sum)) * inv;
+        const f2 minus_m = pack2(-m, -m);
+        sum = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (mask >> k & 1) {
+                f2 v[P];
+                unpack_pairs<E, VEC>(raw[k], v);
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    v[i] = add2(v[i], minus_m);
+                    sum = fma2(v[i], v[i], sum);
+                }
+            }
+        const float r = rsqrtf(fmaf(lane_sum<32>(ln_join(sum)), inv, p.eps));
+        if (lane == 0) {
+            if (p.mean) p.mean[row] = m;
+            if (p.rstd) p.rstd[row] = r;
+        }
+        const f2 r2 = pack2(r, r);
+        E *y = static_cast<E *>(p.out) + row * p.D + lane * VEC;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (mask >> k & 1) {
+                f2 v[P];
+                unpack_pairs<E, VEC>(raw[k], v);
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    const float4 w = ln_smem[(q * K + k) * 32 + lane], b = ln_smem[((Q + q) * K + k) * 32 + lane];
+                    v[2 * q] = fma2(mul2(add2(v[2 * q], minus_m), r2), pack2(w.x, w.y), pack2(b.x, b.y));
+                    v[2 * q + 1] = fma2(mul2(add2(v[2 * q + 1], minus_m), r2), pack2(w.z, w.w), pack2(b.z, b.w));
+                }
+                *reinterpret_cast<Raw *>(y + k * 32 * VEC) = pack_pairs<E, VEC>(v);
+            }
+    }
+}
+
 // R: rows that a team takes at a time.  Two overlap their chains of a wait, sums over the lanes and stores.
 template <typename E, int VEC, int K, int G, int MAXT, int R>
 __global__ void __launch_bounds__(MAXT, G > 0 ? 4 : 1) ln_bwd_kernel(const __grid_constant__ LnParams p) {
@@ -527,7 +605,11 @@ template <typename E, int VEC, bool BWD> cudaError_t ln_run_v(const LnParams &p,
                                                                   cudaStream_t s) {
     constexpr int KM = kLnElems / VEC, KH = kLnBlockElems / VEC, FEW = BWD ? kLnBwdThreads : kLnFwdThreads;
     if (t.g == 0) {
-        if (t.k <= KH) return ln_run<E, VEC, KH, 0, FEW, BWD>(p, t, most, grid, s);
+        // two rows behind one barrier in the backward pass, us, one in brackets: bf16 8,192 x 2,048 29.4 (33.5), x 4,096 51.2
+        // (60.3), fp16 8,000 x 2,052 37 (46.6), fp32 4,096 x 2,048 23.2 (24.8); single elements would lose, fp32 4,099 x
+        // 1,001 19.5 (16.4), and the forward pass, 8,192 x 2,048 19.1 (17.8); 16 elements a thread instead of 8, 36.9
+        constexpr int R = BWD && VEC > 1 && LnAhead<E, VEC, KH, 0, 2>::kAsync ? 2 : 1;
+        if (t.k <= KH) return ln_run<E, VEC, KH, 0, FEW, BWD, R>(p, t, most, grid, s);
         return t.threads <= FEW ? ln_run<E, VEC, KM, 0, FEW, BWD>(p, t, most, grid, s)
                                 : ln_run<E, VEC, KM, 0, kLnMostThreads, BWD>(p, t, most, grid, s);
     }
@@ -555,9 +637,58 @@ template <typename E, int VEC, bool BWD> cudaError_t ln_run_v(const LnParams &p,
     return t.k <= KH ? ln_run<E, VEC, KH, 32, kLnThreads, BWD>(p, t, most, grid, s)
                      : ln_run<E, VEC, KM, 32, kLnThreads, BWD>(p, t, most, grid, s);
 }
+template <typename E, int VEC, int K> cudaError_t ln_run_wide(const LnParams &p, int n_sm, cudaStream_t stream) {
+    constexpr int smem = 2 * 32 * K * VEC * static_cast<int>(sizeof(float));  // at most 32 KB
+    static std::atomic<int> known[64] = {};  // CTAs that an SM holds, asked once per device
+    int dev = 0, per_sm = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    per_sm = known[dev & 63].load(std::memory_order_relaxed);
+    if (per_sm == 0) {
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, ln_fwd_wide_kernel<E, VEC, K>, kLnWideThreads, smem);
+        if (e != cudaSuccess) return e;
+        if (per_sm < 1) return cudaErrorInvalidConfiguration;
+        known[dev & 63].store(per_sm, std::memory_order_relaxed);
+    }
+    constexpr int warps = kLnWideThreads / 32;
+    const long long n = std::min((p.rows + warps - 1) / warps, (long long)n_sm * per_sm);
+    ln_fwd_wide_kernel<E, VEC, K><<<static_cast<unsigned>(n), kLnWideThreads, smem, stream>>>(p);
+    return cudaGetLastError();
+}
+// Whether a warp holds a 16-bit row raw (at most 256 bytes a lane): rows that would take a CTA from four rows an SM on,
+// and rows of a warp where there are 16 to 64 an SM, too few to pay for the rows ahead.  In us,
+// teams in brackets: bf16 8,192 x 1,024 8.7 (11.0), x 2,048 14.3 (17.8), x 4,096 27.9 (32.8), 20,000 x 1,004 17.0 (24.6), fp16
+// 8,192 x 768 7.9 (9.9), 5,000 x 192 3.4 (4.1), 3,000 x 256 3.1 (3.8).  With fewer rows the warps are too few, 512 x 640 3.1 (2.8);
+// many narrow ones 51,200 x 256 16.8 (12.3); fp32, of 128 bytes a lane at 1,024, 8,192 x 1,024 14.6 (13.3).
+template <typename E> bool ln_wide(const LnParams &p, const LnTeam &t, int n_sm) {
+    if (sizeof(E) != 2 || t.vec < 4 || t.g == 8 || p.D > 32 * 128) return false;
+    return t.g == 0 ? p.rows >= 4LL * n_sm : p.rows >= 16LL * n_sm && p.rows <= 64LL * n_sm;
+}
+template <typename E, int VEC> cudaError_t ln_run_wide_k(const LnParams &p, int n_sm, cudaStream_t s) {
+    const int k = ((p.D + VEC - 1) / VEC + 31) / 32;
+    if (k <= 2) return ln_run_wide<E, VEC, 2>(p, n_sm, s);
+    if (k <= 3) return ln_run_wide<E, VEC, 3>(p, n_sm, s);
+    if (k <= 4) return ln_run_wide<E, VEC, 4>(p, n_sm, s);
+    if (k <= 6) return ln_run_wide<E, VEC, 6>(p, n_sm, s);
+    if (k <= 8) return ln_run_wide<E, VEC, 8>(p, n_sm, s);
+    if (k <= 12) return ln_run_wide<E, VEC, 12>(p, n_sm, s);
+    if constexpr (VEC == 4) {
+        if (k > 24) return ln_run_wide<E, VEC, 32>(p, n_sm, s);
+        if (k > 16) return ln_run_wide<E, VEC, 24>(p, n_sm, s);
+    }
+    return ln_run_wide<E, VEC, 16>(p, n_sm, s);
+}
 template <typename E, bool BWD> cudaError_t ln_run_e(const LnParams &p, long long most, int *grid, cudaStream_t s) {
     constexpr int V = 16 / static_cast<int>(sizeof(E));
     const LnTeam t = ln_team(p, sizeof(E), BWD);
+    if constexpr (!BWD && sizeof(E) == 2) {
+        int n_sm = 0;
+        const cudaError_t e = sm_count(&n_sm);
+        if (e != cudaSuccess) return e;
+        if (ln_wide<E>(p, t, n_sm)) {
+            return t.vec == V ? ln_run_wide_k<E, V>(p, n_sm, s) : ln_run_wide_k<E, 4>(p, n_sm, s);
+        }
+    }
     if (t.vec == V) return ln_run_v<E, V, BWD>(p, t, most, grid, s);
     if constexpr (sizeof(E) == 2) {
         if (t.vec == 4) return ln_run_v<E, 4, BWD>(p, t, most, grid, s);

@@ -61,7 +61,8 @@ def _check_forward(x, w, b, out, mean, rstd, what):
 # every team (8 lanes, a warp, a CTA), full and ragged vectors, single elements and single rows
 SHAPES = [(1, 1), (3, 2), (5, 7), (1, 64), (33, 64), (17, 127), (130, 128), (7, 130), (1600, 192), (77, 384), (2, 512),
           (9, 513), (65, 1000), (41, 1001), (3, 4096), (2, 4099), (5, 8192), (1, 16384), (2, 16383),
-          (130, 300), (65, 320), (33, 380), (9, 460), (41, 1004), (3, 8196), (1, 16380), (19, 4), (7, 12)]
+          (130, 300), (65, 320), (33, 380), (9, 460), (41, 1004), (3, 8196), (1, 16380), (19, 4), (7, 12),
+          (701, 640), (613, 1004), (650, 2052), (609, 4096), (620, 4088), (1300, 516), (2500, 384), (2433, 300), (2441, 264)]
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
@@ -118,6 +119,25 @@ def test_a_nan_row_stays_alone():
     keep[[7, 9]] = False
     assert torch.equal(out[keep], clean[keep])
     assert bool(out[7].isnan().all()) and bool(out[9].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,D,stride", [(640, 1000, 2000), (640, 1004, 1012), (700, 2056, 4112), (2500, 384, 1152), (2500, 300, 308)])
+def test_many_strided_rows(rows, D, stride, dtype):
+    """Enough rows for a warp to hold each: strides, no weights, no bias, statistics, and a NaN that stays in its row."""
+    x, _, w, b = _inputs(rows, D, dtype, 11 + D, stride)
+    out, mean, rstd = gla.layernorm(x, None, None, EPS, stats=True)
+    _check_forward(x, None, None, out, mean, rstd, "no affine")
+    _check_forward(x, w, None, gla.layernorm(x, w, None, EPS), None, None, "no bias")
+    clean = gla.layernorm(x, w, b, EPS)
+    _check_forward(x, w, b, clean, None, None, "affine")
+    x[7, 3] = float("nan")
+    x[rows - 1, D - 1] = float("inf")
+    out = gla.layernorm(x, w, b, EPS)
+    keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+    keep[[7, rows - 1]] = False
+    assert torch.equal(out[keep], clean[keep])
+    assert bool(out[7].isnan().all()) and bool(out[rows - 1].isnan().all())
 
 
 def _check_backward(x, dy, w, mean, rstd, dx, dw, db, what):
