@@ -9,8 +9,8 @@
 // difference of moments), and the row is written once.  A row belongs to a team of threads:
 // 8 lanes, a warp or a whole CTA, whichever keeps a thread at 16 elements or fewer, so that
 // it keeps its share of the weights and, in the backward pass, of dw and db beside them for all rows
-// it visits; the next row's loads are issued before the current row's sums.  Many wide 16-bit rows
-// of the forward pass are held by one warp each instead (ln_fwd_wide_kernel).  Each backward
+// it visits; the next row's loads are issued before the current row's sums.  Many rows of the
+// forward pass that no team suits are held by one warp each instead (ln_fwd_wide_kernel).  Each backward
 // CTA then adds its teams' shares in shared memory and writes one partial row; a second
 // kernel adds the partial rows in a fixed order (no atomics: the same bits every time).
 //
@@ -303,28 +303,54 @@ __global__ void __launch_bounds__(MAXT, 1) ln_fwd_kernel(const __grid_constant__
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
+// CTAs of an SM for `bytes` of a row in a lane's registers.
+constexpr int ln_wide_ctas(int bytes) { return bytes <= 64 ? 4 : bytes <= 128 ? 3 : 2; }
 // A row of many elements held by one warp, as stored (up to 256 bytes a lane), so that what a row costs beside its
 // elements is paid by one warp and no barrier is met; the weights lie in shared memory, pieces of four floats in planes
 // that 8 lanes read without a bank conflict.
 template <typename E, int VEC, int K>
-__global__ void __launch_bounds__(kLnWideThreads, K * VEC * sizeof(E) <= 64 ? 4 : K * VEC * sizeof(E) <= 128 ? 3 : 2)
+__global__ void __launch_bounds__(kLnWideThreads, ln_wide_ctas(K * (VEC > 1 ? VEC * static_cast<int>(sizeof(E)) : 4)))
     ln_fwd_wide_kernel(const __grid_constant__ LnParams p) {
-    constexpr int P = VEC / 2, Q = VEC / 4;
+    using T = LnNum<VEC>;
     using Raw = typename Vec<E, VEC>::raw;
-    extern __shared__ float4 ln_smem[];  // [w, b][Q][32 K]
+    constexpr int P = kLnNums<VEC>, S = VEC < 4 ? VEC : 4, Q = VEC / S;  // pieces of S floats
+    extern __shared__ float4 ln_smem[];  // [w, b][Q][32 K][S]
+    float *par = reinterpret_cast<float *>(ln_smem);
     const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    // (pieces of S with their loads side by side: element by element the prologue took about 1 us more)
+#pragma unroll 2
     for (int i = threadIdx.x; i < 32 * K * Q; i += blockDim.x) {
-        const int c = i / Q * VEC + i % Q * 4, to = i % Q * 32 * K + i / Q;
-        float w[4], b[4];
+        const int c = i / Q * VEC + i % Q * S, to = (i % Q * 32 * K + i / Q) * S;
+        float w[S], b[S];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < S; ++j) {
             w[j] = p.w && c + j < p.D ? p.w[c + j] : 1.f;
             b[j] = p.b && c + j < p.D ? p.b[c + j] : 0.f;
         }
-        ln_smem[to] = make_float4(w[0], w[1], w[2], w[3]);
-        ln_smem[32 * K * Q + to] = make_float4(b[0], b[1], b[2], b[3]);
+        if constexpr (S == 4) {
+            *reinterpret_cast<float4 *>(par + to) = make_float4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<float4 *>(par + 32 * K * VEC + to) = make_float4(b[0], b[1], b[2], b[3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < S; ++j) par[to + j] = w[j], par[32 * K * VEC + to + j] = b[j];
+        }
     }
     __syncthreads();
+    auto weights = [&](int k, int which, T(&f)[P]) {
+        const float *from = par + which * 32 * K * VEC;
+        if constexpr (VEC == 1) {
+            f[0] = from[k * 32 + lane];
+        } else if constexpr (VEC == 2) {
+            const float2 a = *reinterpret_cast<const float2 *>(from + 2 * (k * 32 + lane));
+            f[0] = pack2(a.x, a.y);
+        } else {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const float4 a = *reinterpret_cast<const float4 *>(from + 4 * ((q * K + k) * 32 + lane));
+                f[2 * q] = pack2(a.x, a.y), f[2 * q + 1] = pack2(a.z, a.w);
+            }
+        }
+    };
     const float inv = 1.f / static_cast<float>(p.D);
     const uint32_t mask = ln_mask<VEC, K>(lane, 32, p.D);
     for (long long row = (long long)blockIdx.x * warps + (threadIdx.x >> 5); row < p.rows; row += (long long)gridDim.x * warps) {
@@ -333,27 +359,27 @@ __global__ void __launch_bounds__(kLnWideThreads, K * VEC * sizeof(E) <= 64 ? 4 
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (mask >> k & 1) raw[k] = *reinterpret_cast<const Raw *>(x + k * 32 * VEC);
-        f2 sum = 0;
+        T sum = 0;
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (mask >> k & 1) {
-                f2 v[P];
-                unpack_pairs<E, VEC>(raw[k], v);
+                T v[P];
+                ln_widen<E, VEC>(raw[k], v);
 #pragma unroll
-                for (int i = 0; i < P; ++i) sum = add2(sum, v[i]);
+                for (int i = 0; i < P; ++i) sum = ln_add(sum, v[i]);
             }
         const float m = lane_sum<32>(ln_join(sum)) * inv;
-        const f2 minus_m = pack2(-m, -m);
+        const T minus_m = ln_splat<T>(-m);
         sum = 0;
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (mask >> k & 1) {
-                f2 v[P];
-                unpack_pairs<E, VEC>(raw[k], v);
+                T v[P];
+                ln_widen<E, VEC>(raw[k], v);
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    v[i] = add2(v[i], minus_m);
-                    sum = fma2(v[i], v[i], sum);
+                    v[i] = ln_add(v[i], minus_m);
+                    sum = ln_fma(v[i], v[i], sum);
                 }
             }
         const float r = rsqrtf(fmaf(lane_sum<32>(ln_join(sum)), inv, p.eps));
@@ -361,20 +387,18 @@ __global__ void __launch_bounds__(kLnWideThreads, K * VEC * sizeof(E) <= 64 ? 4 
             if (p.mean) p.mean[row] = m;
             if (p.rstd) p.rstd[row] = r;
         }
-        const f2 r2 = pack2(r, r);
+        const T r2 = ln_splat<T>(r);
         E *y = static_cast<E *>(p.out) + row * p.D + lane * VEC;
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (mask >> k & 1) {
-                f2 v[P];
-                unpack_pairs<E, VEC>(raw[k], v);
+                T v[P], w[P], b[P];
+                ln_widen<E, VEC>(raw[k], v);
+                weights(k, 0, w);
+                weights(k, 1, b);
 #pragma unroll
-                for (int q = 0; q < Q; ++q) {
-                    const float4 w = ln_smem[(q * K + k) * 32 + lane], b = ln_smem[((Q + q) * K + k) * 32 + lane];
-                    v[2 * q] = fma2(mul2(add2(v[2 * q], minus_m), r2), pack2(w.x, w.y), pack2(b.x, b.y));
-                    v[2 * q + 1] = fma2(mul2(add2(v[2 * q + 1], minus_m), r2), pack2(w.z, w.w), pack2(b.z, b.w));
-                }
-                *reinterpret_cast<Raw *>(y + k * 32 * VEC) = pack_pairs<E, VEC>(v);
+                for (int i = 0; i < P; ++i) v[i] = ln_fma(ln_mul(ln_add(v[i], minus_m), r2), w[i], b[i]);
+                *reinterpret_cast<Raw *>(y + k * 32 * VEC) = ln_narrow<E, VEC>(v);
             }
     }
 }
@@ -655,38 +679,52 @@ template <typename E, int VEC, int K> cudaError_t ln_run_wide(const LnParams &p,
     ln_fwd_wide_kernel<E, VEC, K><<<static_cast<unsigned>(n), kLnWideThreads, smem, stream>>>(p);
     return cudaGetLastError();
 }
-// Whether a warp holds a 16-bit row raw (at most 256 bytes a lane): rows that would take a CTA from four rows an SM on,
-// and rows of a warp where there are 16 to 64 an SM, too few to pay for the rows ahead.  In us,
-// teams in brackets: bf16 8,192 x 1,024 8.7 (11.0), x 2,048 14.3 (17.8), x 4,096 27.9 (32.8), 20,000 x 1,004 17.0 (24.6), fp16
-// 8,192 x 768 7.9 (9.9), 5,000 x 192 3.4 (4.1), 3,000 x 256 3.1 (3.8).  With fewer rows the warps are too few, 512 x 640 3.1 (2.8);
-// many narrow ones 51,200 x 256 16.8 (12.3); fp32, of 128 bytes a lane at 1,024, 8,192 x 1,024 14.6 (13.3).
+// Whether a warp holds a row raw.  In us, teams in brackets.  16-bit vectors of 8 and 16 bytes, at most 256 bytes a lane:
+// rows that would take a CTA from four an SM on (bf16 8,192 x 1,024 8.7 (11.0), x 2,048 14.3 (17.8), x 4,096 27.9 (32.8), 20,000 x
+// 1,004 17.0 (24.6); 512 x 640 3.1 (2.8)), rows of a warp where there are 16 to 64 an SM, too few to pay for the rows ahead
+// (fp16 5,000 x 192 3.4 (4.1), 3,000 x 256 3.1 (3.8); 51,200 x 256 16.8 (12.3)).  16-bit pairs, from 16 rows an SM on (51,200 x
+// 1,022 43 (76), x 510 24.2 (25.4); 608 x 1,022 3.8 (3.1)), single ones that would take a CTA (51,200 x 955 61 (100); x 511, a
+// warp's, 29.8 (27.7)).  Single fp32 elements, up to 24 a lane, from eight rows an SM on (51,200 x 601 53 (71), x 333 26.0 (33.2),
+// 2,432 x 129 2.7 (3.8); 608 x 601 4.5 (3.8); 32 a lane spill: 4,099 x 1,001 14.7 (13.3)); fp32 vectors lose: 8,192 x 1,024
+// 14.6 (13.3).
 template <typename E> bool ln_wide(const LnParams &p, const LnTeam &t, int n_sm) {
-    if (sizeof(E) != 2 || t.vec < 4 || t.g == 8 || p.D > 32 * 128) return false;
-    return t.g == 0 ? p.rows >= 4LL * n_sm : p.rows >= 16LL * n_sm && p.rows <= 64LL * n_sm;
+    const bool cta = t.g == 0;
+    if (sizeof(E) == 4) return t.vec == 1 && p.D <= 32 * 24 && p.rows >= 8LL * n_sm;
+    if (t.g == 8 || p.D > (t.vec >= 4 ? 32 * 128 : 32 * 32 * t.vec)) return false;
+    if (t.vec < 4) return (cta || t.vec == 2) && p.rows >= 16LL * n_sm;
+    return cta ? p.rows >= 4LL * n_sm : p.rows >= 16LL * n_sm && p.rows <= 64LL * n_sm;
 }
 template <typename E, int VEC> cudaError_t ln_run_wide_k(const LnParams &p, int n_sm, cudaStream_t s) {
     const int k = ((p.D + VEC - 1) / VEC + 31) / 32;
-    if (k <= 2) return ln_run_wide<E, VEC, 2>(p, n_sm, s);
-    if (k <= 3) return ln_run_wide<E, VEC, 3>(p, n_sm, s);
-    if (k <= 4) return ln_run_wide<E, VEC, 4>(p, n_sm, s);
-    if (k <= 6) return ln_run_wide<E, VEC, 6>(p, n_sm, s);
-    if (k <= 8) return ln_run_wide<E, VEC, 8>(p, n_sm, s);
-    if (k <= 12) return ln_run_wide<E, VEC, 12>(p, n_sm, s);
-    if constexpr (VEC == 4) {
-        if (k > 24) return ln_run_wide<E, VEC, 32>(p, n_sm, s);
-        if (k > 16) return ln_run_wide<E, VEC, 24>(p, n_sm, s);
+    if constexpr (VEC > 1 || sizeof(E) == 4) {  // (single 16-bit elements: more than 16 a lane)
+        if (k <= 2) return ln_run_wide<E, VEC, 2>(p, n_sm, s);
+        if (k <= 3) return ln_run_wide<E, VEC, 3>(p, n_sm, s);
+        if (k <= 4) return ln_run_wide<E, VEC, 4>(p, n_sm, s);
+        if (k <= 6) return ln_run_wide<E, VEC, 6>(p, n_sm, s);
+        if (k <= 8) return ln_run_wide<E, VEC, 8>(p, n_sm, s);
+        if (k <= 12) return ln_run_wide<E, VEC, 12>(p, n_sm, s);
+        if (VEC == 8 || k <= 16) return ln_run_wide<E, VEC, 16>(p, n_sm, s);
     }
-    return ln_run_wide<E, VEC, 16>(p, n_sm, s);
+    if constexpr (VEC < 8) {
+        if (sizeof(E) == 4 || k <= 24) return ln_run_wide<E, VEC, 24>(p, n_sm, s);
+        if constexpr (sizeof(E) == 2) return ln_run_wide<E, VEC, 32>(p, n_sm, s);
+    }
+    return cudaErrorInvalidValue;
 }
 template <typename E, bool BWD> cudaError_t ln_run_e(const LnParams &p, long long most, int *grid, cudaStream_t s) {
     constexpr int V = 16 / static_cast<int>(sizeof(E));
     const LnTeam t = ln_team(p, sizeof(E), BWD);
-    if constexpr (!BWD && sizeof(E) == 2) {
+    if constexpr (!BWD) {
         int n_sm = 0;
         const cudaError_t e = sm_count(&n_sm);
         if (e != cudaSuccess) return e;
         if (ln_wide<E>(p, t, n_sm)) {
-            return t.vec == V ? ln_run_wide_k<E, V>(p, n_sm, s) : ln_run_wide_k<E, 4>(p, n_sm, s);
+            if constexpr (sizeof(E) == 2) {
+                if (t.vec == 8) return ln_run_wide_k<E, 8>(p, n_sm, s);
+                if (t.vec == 4) return ln_run_wide_k<E, 4>(p, n_sm, s);
+                if (t.vec == 2) return ln_run_wide_k<E, 2>(p, n_sm, s);
+            }
+            return ln_run_wide_k<E, 1>(p, n_sm, s);
         }
     }
     if (t.vec == V) return ln_run_v<E, V, BWD>(p, t, most, grid, s);

@@ -62,7 +62,8 @@ def _check_forward(x, w, b, out, mean, rstd, what):
 SHAPES = [(1, 1), (3, 2), (5, 7), (1, 64), (33, 64), (17, 127), (130, 128), (7, 130), (1600, 192), (77, 384), (2, 512),
           (9, 513), (65, 1000), (41, 1001), (3, 4096), (2, 4099), (5, 8192), (1, 16384), (2, 16383),
           (130, 300), (65, 320), (33, 380), (9, 460), (41, 1004), (3, 8196), (1, 16380), (19, 4), (7, 12),
-          (701, 640), (613, 1004), (650, 2052), (609, 4096), (620, 4088), (1300, 516), (2500, 384), (2433, 300), (2441, 264)]
+          (701, 640), (613, 1004), (650, 2052), (609, 4096), (620, 4088), (1300, 516), (2500, 384), (2433, 300), (2441, 264),
+          (2433, 955), (2440, 1022), (2500, 2046), (2437, 510), (2500, 514), (1300, 1), (1217, 33), (1301, 129), (1220, 333), (1219, 767)]
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
@@ -121,8 +122,9 @@ def test_a_nan_row_stays_alone():
     assert bool(out[7].isnan().all()) and bool(out[9].isnan().all())
 
 
-@pytest.mark.parametrize("dtype", ["f16", "bf16"])
-@pytest.mark.parametrize("rows,D,stride", [(640, 1000, 2000), (640, 1004, 1012), (700, 2056, 4112), (2500, 384, 1152), (2500, 300, 308)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("rows,D,stride", [(640, 1000, 2000), (640, 1004, 1012), (700, 2056, 4112), (2500, 384, 1152), (2500, 300, 308),
+                                           (2500, 955, 957), (2500, 1022, 1030), (1300, 333, 335)])
 def test_many_strided_rows(rows, D, stride, dtype):
     """Enough rows for a warp to hold each: strides, no weights, no bias, statistics, and a NaN that stays in its row."""
     x, _, w, b = _inputs(rows, D, dtype, 11 + D, stride)
